@@ -62,7 +62,7 @@ typedef enum {
   CAFEQ_ERR_WORKSPACE = -7    /* ws is NULL or smaller than cafeq_workspace_bytes() */
 } cafeq_status;
 
-typedef enum { CAFEQ_F32 = 0, CAFEQ_BF16 = 1 } cafeq_dtype;
+typedef enum { CAFEQ_F32 = 0, CAFEQ_BF16 = 1, CAFEQ_I8 = 2 /* activations of cafeq_infer_packed only */ } cafeq_dtype;
 typedef enum { CAFEQ_AXIS_COL = 0, CAFEQ_AXIS_ROW = 1 } cafeq_axis;
 typedef enum { CAFEQ_SIDE_T = 0, CAFEQ_SIDE_TINV = 1 } cafeq_side;
 typedef enum { CAFEQ_Q_SYM_ABSMAX = 0, CAFEQ_Q_ASYM_MINMAX = 1 } cafeq_qmode;
@@ -208,6 +208,61 @@ size_t cafeq_infer_workspace_bytes(int n, int64_t in);
 int cafeq_infer_single(const float* X, int n, int64_t ldx, const cafeq_xform* xf, const int8_t* codes,
                        const float* scales, int64_t out, int64_t in, int group, float* Y, int64_t ldy,
                        void* ws, void* stream);
+
+/* ---- Serving a quantized layer: activations in 8 bits, weights in 4 -----------------------
+ *
+ * cafeq_norm_quantize makes the activations of a quantized layer ready (X M^-1 of the display in paper Sec. 4.1,
+ * with the norm before it and the rounding after it):
+ *   h = x + residual                                     (n rows of d; without a residual h = x)
+ *   y = h * (mean_c h_c^2 + eps)^-1/2 * (gain_offset + gain_c)        (y = h where in->norm is 0; gain NULL: factor 1)
+ *   z[b*k + i] = sum_j Tinv[b][i][j] y[b*k + j]          (z = y where xf is NULL; only Tinv, k, nb of it are read)
+ *   a = max |z| over a group, inv = min(fl(127 / a), FLT_MAX), q = rint(fl(z*inv)), scale = fl(a / 127)
+ * x, residual, sum: float32 or bfloat16 (one type), leading dimensions in elements; sum (may be NULL) receives h, rounded
+ * once; all arithmetic is float32 on the unrounded h.  codes int8 [n][d] dense, scales float32 [n][d/group]
+ * (group 0: one a row; else a multiple of 32 that divides d); both NULL: no codes.  values (may be NULL if codes
+ * is not; float32 or bfloat16, leading dimension ldv): fl(q*scale), the values the codes stand for, or z where no codes are
+ * asked for.  A group of zeros has scale 0 and codes 0; one that holds an infinity or a NaN has codes 0 and that
+ * magnitude as its scale, so that whatever reads it is not finite.  n = 0 does nothing; d up to 65536.
+ * xf NULL: any d, strides and alignments (rows that start at multiples of 16 bytes with d a multiple of 8 are
+ * faster); sum may be x or residual itself.  With xf: k in {32, 64, 128, 256}, nb*k == d, rep == 1; rows of x, residual
+ * and values start at multiples of 16 bytes (as do gain and Tinv), sum may overlap neither x nor residual
+ * (CAFEQ_ERR_INVALID_ARG), and ws holds cafeq_norm_workspace_bytes(n, d, xf, group) bytes, 16-byte aligned (group < 0: no
+ * codes). */
+typedef struct {
+  const void* x;
+  const void* residual;
+  void* sum;
+  int64_t ldx, ldr, lds;
+  int32_t dtype;          /* cafeq_dtype of x, residual and sum */
+  int32_t norm;           /* 0: no norm */
+  const float* gain;      /* [d] or NULL */
+  float gain_offset, eps;
+} cafeq_activations;
+size_t cafeq_norm_workspace_bytes(int64_t n, int64_t d, const cafeq_xform* xf, int64_t group);
+int cafeq_norm_quantize(const cafeq_activations* in, int64_t n, int64_t d, const cafeq_xform* xf, int64_t group,
+                        int8_t* codes, float* scales, void* values, int values_dtype, int64_t ldv, void* ws,
+                        void* stream);
+
+/* Weights with codes of up to 4 bits, packed once for cafeq_infer_packed.  codes int8 [out][in] in [-8, 7] (the lower four bits
+ * are kept) and scales float32 [out][in/group] as written by cafeq_rtn_quantize and the loss calls on CAFEQ_AXIS_COL
+ * (group 0 = the whole line; in and group multiples of 32, in <= 65536).  packed: cafeq_packed_bytes(out, in, group)
+ * bytes (0 on invalid sizes), 16-byte aligned: half a byte a weight in the order the matrix instructions take them, rows
+ * rounded up to 32 and columns to 128, then the scales.  The layout belongs to the build of the library that wrote it. */
+size_t cafeq_packed_bytes(int64_t out, int64_t in, int64_t group);
+int cafeq_pack_nibbles(const int8_t* codes, const float* scales, int64_t out, int64_t in, int64_t group,
+                       void* packed, void* stream);
+
+/* Y[t][o] = sum_c scales[o][c/group] codes[o][c] x[t][c] for packed weights: the layer of cafeq_infer_single at half its bytes,
+ * for one token or many.  X [n][in], leading dimension ldx (rows start at multiples of 16 bytes), x_type:
+ *   CAFEQ_F32, CAFEQ_BF16   the activations (already through the transform); xscales NULL, xgroup ignored
+ *   CAFEQ_I8                codes of cafeq_norm_quantize with their scales xscales [n][in/xgroup] (xgroup 0: one a token;
+ *                           else a multiple of 32 that divides in)
+ * Y float32 or bfloat16 [n][out], leading dimension ldy >= out.  Sums over a group are exact integers with CAFEQ_I8 and
+ * float32 otherwise (no activation is rounded); groups are added in float32 in a fixed order, and one rounding leads to Y.
+ * n = 0 does nothing; n up to 2^20. */
+int cafeq_infer_packed(const void* X, int x_type, int64_t n, int64_t ldx, const float* xscales, int64_t xgroup,
+                       const void* packed, int64_t out, int64_t in, int64_t group, void* Y, int y_dtype,
+                       int64_t ldy, void* stream);
 
 /* Z = W.blockdiag(X) or blockdiag(X).W with X = T (CAFEQ_SIDE_T) or Tinv
  * (CAFEQ_SIDE_TINV)  (paper Sec. 4.1 block-diagonal M; Sec. 4.2 U = W1 M, V = M^-1 W2).

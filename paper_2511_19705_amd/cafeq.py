@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -17,7 +18,7 @@ LIB_PATH = os.environ.get("CAFEQ_LIBRARY", os.path.join(_HERE, "libcafeq.so"))
 AXIS_COL, AXIS_ROW = 0, 1
 Q_SYM, Q_MINMAX = 0, 1   # the symmetric absmax grid; the min/max grid of the paper's Eq. (1)
 SIDE_T, SIDE_TINV = 0, 1
-F32, BF16 = 0, 1
+F32, BF16, I8 = 0, 1, 2   # I8: activations of infer_packed only
 CALL_RTN, CALL_PROXY, CALL_DUAL, CALL_ADAPTIVE = 0, 1, 2, 3
 
 EXPORTS = (
@@ -27,7 +28,8 @@ EXPORTS = (
     "cafeq_orth_penalty", "cafeq_sgd_update", "cafeq_adam_update", "cafeq_optimize_single",
     "cafeq_optimize_pair", "cafeq_pqe", "cafeq_rtn_quantize_minmax", "cafeq_hadamard_rtn", "cafeq_hadamard_workspace_bytes",
     "cafeq_infer_single", "cafeq_infer_workspace_bytes", "cafeq_set_launch_timing", "cafeq_rtn_quantize_static", "cafeq_prepared_bytes", "cafeq_prepare_weights",
-    "cafeq_stream_read_probe",
+    "cafeq_stream_read_probe", "cafeq_norm_quantize", "cafeq_norm_workspace_bytes", "cafeq_packed_bytes", "cafeq_pack_nibbles",
+    "cafeq_infer_packed",
 )
 
 
@@ -60,6 +62,12 @@ class OptCfg(ctypes.Structure):
     _fields_ = [("steps", ctypes.c_int32), ("lr", ctypes.c_float), ("lambda_orth", ctypes.c_float),
                 ("normalize", ctypes.c_int32), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
                 ("eps", ctypes.c_double)]
+
+
+class Activations(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("sum", ctypes.c_void_p), ("ldx", ctypes.c_int64),
+                ("ldr", ctypes.c_int64), ("lds", ctypes.c_int64), ("dtype", ctypes.c_int32), ("norm", ctypes.c_int32),
+                ("gain", ctypes.c_void_p), ("gain_offset", ctypes.c_float), ("eps", ctypes.c_float)]
 
 
 def _load():
@@ -110,8 +118,14 @@ def _load():
                               vp, vp, vp]
     lib.cafeq_set_launch_timing.argtypes = [ctypes.POINTER(LaunchTiming)]
     lib.cafeq_stream_read_probe.argtypes = [vp, ctypes.c_size_t, vp, vp]
+    lib.cafeq_norm_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(Xform), i64]
+    lib.cafeq_norm_quantize.argtypes = [ctypes.POINTER(Activations), i64, i64, ctypes.POINTER(Xform), i64, vp, vp, vp, i32,
+                                        i64, vp, vp]
+    lib.cafeq_packed_bytes.argtypes = [i64, i64, i64]
+    lib.cafeq_pack_nibbles.argtypes = [vp, vp, i64, i64, i64, vp, vp]
+    lib.cafeq_infer_packed.argtypes = [vp, i32, i64, i64, vp, i64, vp, i64, i64, i64, vp, i32, i64, vp]
     for n in EXPORTS[3:]:
-        getattr(lib, n).restype = i32
+        getattr(lib, n).restype = ctypes.c_size_t if n.endswith("_bytes") else i32
     return lib
 
 
@@ -492,3 +506,135 @@ def infer_single(X, Tinv, codes, scales, group, out=None):
     _check(lib.cafeq_infer_single(_ptr(X), n, X.stride(0), xfp, _ptr(codes), _ptr(scales), O, d, group, _ptr(Y),
                                   Y.stride(0), _ptr(ws), _stream()))
     return Y
+
+
+_FLOATS = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _rows(t, what):
+    """A 2-D tensor on the current device with unit column stride: its leading dimension."""
+    if t.dim() != 2 or not t.is_cuda or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise CafeqError("%s: need a 2-D CUDA tensor with unit column stride" % what)
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise CafeqError("%s: on another device than the current one" % what)
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+
+
+def _like(t, x, dtypes, shape, what):
+    """Checks an operand that goes with x: on its device, of one of the types, contiguous, of this shape."""
+    if t.device != x.device or t.dtype not in dtypes or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise CafeqError("%s: need a contiguous tensor %s of %s on %s" % (what, tuple(shape), dtypes, x.device))
+
+
+class Normed(NamedTuple):
+    """What norm_quantize returns; None for what was not asked for."""
+    codes: Optional[torch.Tensor]
+    scales: Optional[torch.Tensor]
+    values: Optional[torch.Tensor]
+    sum: Optional[torch.Tensor]
+
+
+def norm_quantize(X, gain=None, residual=None, eps=1e-6, gain_offset=0.0, norm=True, Tinv=None, group=0, values=None,
+                  sum_out=None):
+    """cafeq_norm_quantize: residual addition, root-mean-square norm (norm=False: none), the transform's inverse blocks Tinv and
+    8 bits with a scale per `group` columns (0: per row; None: no codes).  X, residual [n][d] float32 or bfloat16.
+    values: None, or the type of a tensor that receives what the codes stand for (without codes: the result itself).
+    The sum X + residual is returned where a residual is given, in sum_out if that is given too (which without Tinv may be X or
+    residual)."""
+    if X.dtype not in _FLOATS:
+        raise CafeqError("X must be float32 or bfloat16")
+    if values is not None and values not in _FLOATS:
+        raise CafeqError("values must be torch.float32 or torch.bfloat16")
+    if group is None and values is None:
+        raise CafeqError("neither codes nor values are asked for")
+    n, d = X.shape
+    dev = X.device
+    a = Activations(x=X.data_ptr(), ldx=_rows(X, "X"), dtype=_FLOATS[X.dtype], norm=1 if norm else 0, gain_offset=gain_offset, eps=eps)
+    if gain is not None:
+        _like(gain, X, (torch.float32,), (d,), "gain")
+        a.gain = gain.data_ptr()
+    if residual is not None:
+        if residual.shape != X.shape or residual.dtype != X.dtype or residual.device != dev:
+            raise CafeqError("residual must have the shape, type and device of X")
+        a.residual, a.ldr = residual.data_ptr(), _rows(residual, "residual")
+        if sum_out is None:
+            sum_out = torch.empty((n, d), dtype=X.dtype, device=dev)
+    if sum_out is not None:
+        if sum_out.shape != X.shape or sum_out.dtype != X.dtype or sum_out.device != dev:
+            raise CafeqError("sum_out must have the shape, type and device of X")
+        a.sum, a.lds = sum_out.data_ptr(), _rows(sum_out, "sum_out")
+    codes = scales = out = xf = ws = None
+    g = -1
+    if group is not None:
+        g = group or d
+        if g < 1 or d % g:
+            raise CafeqError("group must divide the columns")
+        codes = torch.empty((n, d), dtype=torch.int8, device=dev)
+        scales = torch.empty((n, d // g), dtype=torch.float32, device=dev)
+        g = group
+    if values is not None:
+        out = torch.empty((n, d), dtype=values, device=dev)
+    if Tinv is not None:
+        if Tinv.dim() != 3 or Tinv.shape[1] != Tinv.shape[2]:
+            raise CafeqError("Tinv must be [nb][k][k]")
+        _like(Tinv, X, (torch.float32,), Tinv.shape, "Tinv")
+        xf = Xform(None, Tinv.data_ptr(), Tinv.shape[1], Tinv.shape[0], 1)
+        # of this call alone: calls on several streams at once share nothing
+        ws = torch.empty(int(lib.cafeq_norm_workspace_bytes(n, d, ctypes.byref(xf), g)), dtype=torch.uint8, device=dev)
+    if n:
+        _check(lib.cafeq_norm_quantize(ctypes.byref(a), n, d, ctypes.byref(xf) if xf else None, max(g, 0), _ptr(codes), _ptr(scales),
+                                       _ptr(out), _FLOATS.get(values, F32), d, _ptr(ws), _stream()))
+    return Normed(codes, scales, out, sum_out)
+
+
+class PackedWeight(NamedTuple):
+    """Weights packed by pack_nibbles: the buffer and what it was made from."""
+    data: torch.Tensor
+    rows: int
+    cols: int
+    group: int
+
+
+def pack_nibbles(codes, scales, group):
+    """Codes of up to 4 bits and their scales (AXIS_COL, as rtn_quantize returns them) packed for infer_packed."""
+    if codes.dim() != 2 or not codes.is_cuda or codes.dtype != torch.int8 or not codes.is_contiguous():
+        raise CafeqError("codes must be a contiguous 2-D int8 CUDA tensor")
+    rows, cols = codes.shape
+    nbytes = int(lib.cafeq_packed_bytes(rows, cols, group))
+    if nbytes == 0:
+        raise CafeqError("cannot pack codes of this shape (columns and group must be multiples of 32, the group a divisor)")
+    _like(scales, codes, (torch.float32,), _scale_shape(rows, cols, group, AXIS_COL), "scales")
+    buf = torch.empty(nbytes, dtype=torch.uint8, device=codes.device)
+    _check(lib.cafeq_pack_nibbles(_ptr(codes), _ptr(scales), rows, cols, group, _ptr(buf), _stream()))
+    return PackedWeight(buf, rows, cols, group)
+
+
+_ACTIVATIONS = {torch.float32: F32, torch.bfloat16: BF16, torch.int8: I8}
+
+
+def infer_packed(X, weight, xscales=None, xgroup=0, dtype=torch.float32, out=None):
+    """Y[n][rows] = X . dequant(weight)^T (cafeq_infer_packed).  X float32 or bfloat16, or the int8 codes of norm_quantize with their
+    scales and group; Y in `dtype` (float32 or bfloat16), or in `out`."""
+    if X.dtype not in _ACTIVATIONS:
+        raise CafeqError("X must be float32, bfloat16 or int8")
+    ldx = _rows(X, "X")
+    n, d = X.shape
+    if d != weight.cols or weight.data.device != X.device:
+        raise CafeqError("X must have the columns (%d) and the device of the weight" % weight.cols)
+    if X.dtype == torch.int8:
+        if xscales is None or xgroup < 0 or d % (xgroup or d):
+            raise CafeqError("int8 activations need their scales and a group that divides the columns")
+        _like(xscales, X, (torch.float32,), (n, d // (xgroup or d)), "xscales")
+    elif xscales is not None:
+        raise CafeqError("xscales go with int8 activations")
+    if out is None:
+        out = torch.empty((n, weight.rows), dtype=dtype, device=X.device)
+    elif tuple(out.shape) != (n, weight.rows) or out.device != X.device:
+        raise CafeqError("out must be [%d][%d] on the device of X" % (n, weight.rows))
+    if out.dtype not in _FLOATS:
+        raise CafeqError("Y must be float32 or bfloat16")
+    ldy = _rows(out, "out")
+    if n:
+        _check(lib.cafeq_infer_packed(_ptr(X), _ACTIVATIONS[X.dtype], n, ldx, _ptr(xscales), xgroup, _ptr(weight.data), weight.rows, d,
+                                      weight.group, _ptr(out), _FLOATS[out.dtype], ldy, _stream()))
+    return out

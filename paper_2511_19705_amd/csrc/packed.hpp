@@ -1,0 +1,146 @@
+// Packed 4-bit weights: the layout, and the activations' forms on the matrix cores.
+#pragma once
+#include "cafeq_common.hpp"
+
+namespace cafeq {
+
+using i32x4 = __attribute__((__vector_size__(4 * sizeof(int)))) int;
+using f32x4 = __attribute__((__vector_size__(4 * sizeof(float)))) float;
+using bf16x8_t = __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16;
+
+// Codes: tiles of 16 rows x 128 columns, 1 KB each, [row tile][block of 128 columns][lane][16 bytes].  Lane l of a tile holds row
+// l % 16 and, in pair j of its two eight-byte pairs, the columns 64 j + 16 (l / 16) + 0 .. 15; byte b of dword e of a pair holds
+// column 8 e + b in its lower half and 8 e + 4 + b in its upper one.  A wave's load of a tile is 1 KB side by side, and a lane's
+// pair unpacks to 16 consecutive columns, the K range of the 8-bit matrix instructions' lane.
+// Scales behind them: [row tile][group][16 rows] float32.  Rows beyond the matrix and columns beyond its width are zeros.
+constexpr int kRowTile = 16, kBlockK = 128;
+
+struct PackedShape {
+  int64_t rows, cols, group, groups, row_tiles, kblocks, scales_at, bytes;
+};
+
+inline int packed_shape(int64_t out, int64_t in, int64_t group, PackedShape* p) {
+  if (out < 1 || in < 32 || in % 32 != 0 || group < 0) return CAFEQ_ERR_BAD_SHAPE;
+  const int64_t g = group == 0 ? in : group;
+  if (g % 32 != 0 || in % g != 0) return CAFEQ_ERR_BAD_SHAPE;
+  if (in > 65536 || out > (int64_t(1) << 24)) return CAFEQ_ERR_UNSUPPORTED;   // integer sums of a group stay below 2^31
+  p->rows = out;
+  p->cols = in;
+  p->group = g;
+  p->groups = in / g;
+  p->row_tiles = (out + 2 * kRowTile - 1) / (2 * kRowTile) * 2;   // whole tiles of 32 rows
+  p->kblocks = (in + kBlockK - 1) / kBlockK;
+  p->scales_at = p->row_tiles * p->kblocks * 1024;
+  p->bytes = p->scales_at + p->row_tiles * p->groups * kRowTile * int64_t(sizeof(float));
+  return CAFEQ_OK;
+}
+
+__device__ __forceinline__ uint32_t low16(uint32_t w) { return (w << 4) & 0xF0F0F0F0u; }   // 16 q of columns 0 .. 3 of a dword
+__device__ __forceinline__ uint32_t high16(uint32_t w) { return w & 0xF0F0F0F0u; }         // of columns 4 .. 7
+
+// two signed bytes of a dword as bfloat16 (whole numbers up to 128: exact)
+template <int I>
+__device__ __forceinline__ uint32_t bf16_pair(uint32_t w) {
+  const float a = float(int(int8_t(w >> (8 * I)))), b = float(int(int8_t(w >> (8 * I + 8))));
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+// eight codes times 16 as a bfloat16 operand
+__device__ __forceinline__ bf16x8_t bf16_codes(uint32_t w) {
+  const uint32_t lo = low16(w), hi = high16(w);
+  union { uint32_t u[4]; bf16x8_t v; } f;
+  f.u[0] = bf16_pair<0>(lo); f.u[1] = bf16_pair<2>(lo); f.u[2] = bf16_pair<0>(hi); f.u[3] = bf16_pair<2>(hi);
+  return f.v;
+}
+
+// two float32 values' leading bits as a pair of bfloat16, and what they leave (nothing of an infinity)
+__device__ __forceinline__ uint32_t split_pair(float& a, float& b) {
+  const uint32_t ha = __float_as_uint(a) & 0xFFFF0000u, hb = __float_as_uint(b) & 0xFFFF0000u;
+  const float fa = __uint_as_float(ha), fb = __uint_as_float(hb);
+  const uint32_t p = __builtin_amdgcn_perm(hb, ha, 0x07060302u);
+  a = a == fa ? 0.f : a - fa;
+  b = b == fb ? 0.f : b - fb;
+  return p;
+}
+
+__device__ __forceinline__ void store_y(void* y, int dtype, int64_t at, float v) {
+  if (dtype == CAFEQ_F32) { static_cast<float*>(y)[at] = v; return; }
+  const uint32_t u = __float_as_uint(v);
+  static_cast<uint16_t*>(y)[at] =
+      (u & 0x7FFFFFFFu) > 0x7F800000u ? uint16_t((u >> 16) | 0x40u) : uint16_t((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16);
+}
+
+// The forms of the activations.  Chunk: 16 consecutive columns of a token (a lane's share of 64); mul: 64 columns of 16 rows times
+// 16 tokens onto acc, the weights' two dwords of the same columns.
+struct XI8 {
+  static constexpr bool kScaled = true;
+  using Acc = i32x4;
+  struct Chunk { i32x4 v; };
+  static __device__ __forceinline__ Chunk load(const void* x, int64_t at, bool in) {
+    Chunk c;
+    c.v = in ? *reinterpret_cast<const i32x4*>(static_cast<const int8_t*>(x) + at) : i32x4{0, 0, 0, 0};
+    return c;
+  }
+  static __device__ __forceinline__ Chunk keep(const Chunk& c, bool yes) { return yes ? c : Chunk{i32x4{0, 0, 0, 0}}; }
+  static __device__ __forceinline__ void mul(Acc& acc, uint32_t w0, uint32_t w1, const Chunk& c) {
+    const i32x4 a = {int(low16(w0)), int(high16(w0)), int(low16(w1)), int(high16(w1))};
+    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, c.v, acc, 0, 0, 0);
+  }
+  static __device__ __forceinline__ float value(const Acc& acc, int r) { return float(acc[r]); }
+};
+
+struct XBf16 {
+  static constexpr bool kScaled = false;
+  using Acc = f32x4;
+  struct Chunk { bf16x8_t v[2]; };
+  static __device__ __forceinline__ Chunk load(const void* x, int64_t at, bool in) {
+    Chunk c;
+    const bf16x8_t* p = reinterpret_cast<const bf16x8_t*>(static_cast<const uint16_t*>(x) + at);
+    c.v[0] = in ? p[0] : bf16x8_t{};
+    c.v[1] = in ? p[1] : bf16x8_t{};
+    return c;
+  }
+  static __device__ __forceinline__ Chunk keep(const Chunk& c, bool yes) { return yes ? c : Chunk{}; }
+  static __device__ __forceinline__ void mul(Acc& acc, uint32_t w0, uint32_t w1, const Chunk& c) {
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_codes(w0), c.v[0], acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_codes(w1), c.v[1], acc, 0, 0, 0);
+  }
+  static __device__ __forceinline__ float value(const Acc& acc, int r) { return acc[r]; }
+};
+
+struct XF32 {
+  static constexpr bool kScaled = false;
+  using Acc = f32x4;
+  struct Chunk { float v[16]; };
+  static __device__ __forceinline__ Chunk load(const void* x, int64_t at, bool in) {
+    Chunk c;
+    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(x) + at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 f = in ? p[i] : make_float4(0.f, 0.f, 0.f, 0.f);
+      c.v[4 * i] = f.x; c.v[4 * i + 1] = f.y; c.v[4 * i + 2] = f.z; c.v[4 * i + 3] = f.w;
+    }
+    return c;
+  }
+  static __device__ __forceinline__ Chunk keep(const Chunk& c, bool yes) { return yes ? c : Chunk{}; }
+  // three parts of every activation, hi + mid + lo exactly, the small ones first
+  static __device__ __forceinline__ void mul(Acc& acc, uint32_t w0, uint32_t w1, const Chunk& c) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      union { uint32_t u[4]; bf16x8_t v; } part[3];
+      float r[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[i] = c.v[8 * e + i];
+#pragma unroll
+      for (int s = 0; s < 3; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[s].u[i] = split_pair(r[2 * i], r[2 * i + 1]);
+      const bf16x8_t w = bf16_codes(e ? w1 : w0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, part[2].v, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, part[1].v, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, part[0].v, acc, 0, 0, 0);
+    }
+  }
+  static __device__ __forceinline__ float value(const Acc& acc, int r) { return acc[r]; }
+};
+
+}  // namespace cafeq
