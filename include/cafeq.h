@@ -259,10 +259,11 @@ int cafeq_pack_nibbles(const int8_t* codes, const float* scales, int64_t out, in
  *                           else a multiple of 32 that divides in)
  * Y float32 or bfloat16 [n][out], leading dimension ldy >= out.  Sums over a group are exact integers with CAFEQ_I8 and
  * float32 otherwise (no activation is rounded); groups are added in float32 in a fixed order, and one rounding leads to Y.
- * n = 0 does nothing; n up to 2^20. */
+ * n = 0 does nothing; n up to 2^20, ldx up to 2^24.  ws: cafeq_infer_packed_workspace_bytes() bytes (0 for few tokens), 16-byte aligned. */
+size_t cafeq_infer_packed_workspace_bytes(int x_type, int64_t n, int64_t out, int64_t in, int64_t group);
 int cafeq_infer_packed(const void* X, int x_type, int64_t n, int64_t ldx, const float* xscales, int64_t xgroup,
                        const void* packed, int64_t out, int64_t in, int64_t group, void* Y, int y_dtype,
-                       int64_t ldy, void* stream);
+                       int64_t ldy, void* ws, void* stream);
 
 /* Z = W.blockdiag(X) or blockdiag(X).W with X = T (CAFEQ_SIDE_T) or Tinv
  * (CAFEQ_SIDE_TINV)  (paper Sec. 4.1 block-diagonal M; Sec. 4.2 U = W1 M, V = M^-1 W2).

@@ -29,7 +29,7 @@ EXPORTS = (
     "cafeq_optimize_pair", "cafeq_pqe", "cafeq_rtn_quantize_minmax", "cafeq_hadamard_rtn", "cafeq_hadamard_workspace_bytes",
     "cafeq_infer_single", "cafeq_infer_workspace_bytes", "cafeq_set_launch_timing", "cafeq_rtn_quantize_static", "cafeq_prepared_bytes", "cafeq_prepare_weights",
     "cafeq_stream_read_probe", "cafeq_norm_quantize", "cafeq_norm_workspace_bytes", "cafeq_packed_bytes", "cafeq_pack_nibbles",
-    "cafeq_infer_packed",
+    "cafeq_infer_packed", "cafeq_infer_packed_workspace_bytes",
 )
 
 
@@ -123,7 +123,8 @@ def _load():
                                         i64, vp, vp]
     lib.cafeq_packed_bytes.argtypes = [i64, i64, i64]
     lib.cafeq_pack_nibbles.argtypes = [vp, vp, i64, i64, i64, vp, vp]
-    lib.cafeq_infer_packed.argtypes = [vp, i32, i64, i64, vp, i64, vp, i64, i64, i64, vp, i32, i64, vp]
+    lib.cafeq_infer_packed.argtypes = [vp, i32, i64, i64, vp, i64, vp, i64, i64, i64, vp, i32, i64, vp, vp]
+    lib.cafeq_infer_packed_workspace_bytes.argtypes = [i32, i64, i64, i64, i64]
     for n in EXPORTS[3:]:
         getattr(lib, n).restype = ctypes.c_size_t if n.endswith("_bytes") else i32
     return lib
@@ -635,6 +636,9 @@ def infer_packed(X, weight, xscales=None, xgroup=0, dtype=torch.float32, out=Non
         raise CafeqError("Y must be float32 or bfloat16")
     ldy = _rows(out, "out")
     if n:
-        _check(lib.cafeq_infer_packed(_ptr(X), _ACTIVATIONS[X.dtype], n, ldx, _ptr(xscales), xgroup, _ptr(weight.data), weight.rows, d,
-                                      weight.group, _ptr(out), _FLOATS[out.dtype], ldy, _stream()))
+        kind = _ACTIVATIONS[X.dtype]
+        nbytes = lib.cafeq_infer_packed_workspace_bytes(kind, n, weight.rows, d, weight.group)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=X.device) if nbytes else None   # of this call alone
+        _check(lib.cafeq_infer_packed(_ptr(X), kind, n, ldx, _ptr(xscales), xgroup, _ptr(weight.data), weight.rows, d,
+                                      weight.group, _ptr(out), _FLOATS[out.dtype], ldy, _ptr(ws), _stream()))
     return out

@@ -35,6 +35,25 @@ inline int packed_shape(int64_t out, int64_t in, int64_t group, PackedShape* p) 
   return CAFEQ_OK;
 }
 
+// A checked call of cafeq_infer_packed
+struct PackedCall {
+  const uint8_t* packed;
+  PackedShape p;
+  const void* x;
+  int x_type;
+  int64_t n, ldx;
+  const float* xscales;   // [n][xgroups], 8-bit activations
+  int64_t xgroups;
+  int fg;                 // columns a unit: sums start anew there and take their scales
+  int wunits, xunits;     // units a scale of the weights, of the activations
+  void* y;
+  int64_t ldy;
+  int ydtype;
+};
+// packed_gemm.hip: many tokens
+size_t packed_gemm_bytes(int x_type, int64_t n, const PackedShape& p);
+int launch_packed_gemm(const PackedCall& c, void* ws, hipStream_t st);
+
 __device__ __forceinline__ uint32_t low16(uint32_t w) { return (w << 4) & 0xF0F0F0F0u; }   // 16 q of columns 0 .. 3 of a dword
 __device__ __forceinline__ uint32_t high16(uint32_t w) { return w & 0xF0F0F0F0u; }         // of columns 4 .. 7
 

@@ -41,26 +41,12 @@ __global__ __launch_bounds__(256) void pack_kernel(const int8_t* __restrict__ co
   }
 }
 
-struct SmallArgs {
-  const uint8_t* packed;
-  PackedShape p;
-  const void* x;
-  int64_t ldx;
-  const float* xscales;   // [n][xgroups]
-  int64_t xgroups;
-  int wunits, xunits;     // units (of FG columns) a weight's, an activation's scale
-  int64_t n;
-  void* y;
-  int64_t ldy;
-  int ydtype;
-};
-
 // A workgroup owns 16 rows of the weight and 16 TT tokens; its waves share the columns, 128 at a time, and add up through LDS.
 // v_mfma 16x16: A the codes (16 rows), B the activations (16 tokens): a lane has four rows of one token, whose scales are one
 // 16-byte load.  Sums start anew every FG columns (the common divisor of both groups and 128) and are taken up in float32 with
 // their scales.
 template <class X, int TT, int FG>
-__global__ __launch_bounds__(1024) void packed_small_kernel(const SmallArgs a) {
+__global__ __launch_bounds__(1024) void packed_small_kernel(const PackedCall a) {
   extern __shared__ float red[];
   const int tid = threadIdx.x, lane = tid & 63, nwave = blockDim.x >> 6;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -130,12 +116,12 @@ __global__ __launch_bounds__(1024) void packed_small_kernel(const SmallArgs a) {
 }
 
 template <class X, int TT>
-int launch_small_tt(const SmallArgs& a, int fg, hipStream_t st) {
+int launch_small_tt(const PackedCall& a, hipStream_t st) {
   const int64_t nkb = a.p.kblocks;
   const int nw = int(std::min<int64_t>(16, std::max<int64_t>(1, nkb / 2)));
   const dim3 grid(unsigned((a.p.rows + kRowTile - 1) / kRowTile), unsigned((a.n + 16 * TT - 1) / (16 * TT)));
   const size_t lds = size_t(nw) * TT * 1024;
-  switch (fg) {
+  switch (a.fg) {
     case 128: hipLaunchKernelGGL((packed_small_kernel<X, TT, 128>), grid, dim3(nw * 64), lds, st, a); break;
     case 64: hipLaunchKernelGGL((packed_small_kernel<X, TT, 64>), grid, dim3(nw * 64), lds, st, a); break;
     default: hipLaunchKernelGGL((packed_small_kernel<X, TT, 32>), grid, dim3(nw * 64), lds, st, a); break;
@@ -145,9 +131,12 @@ int launch_small_tt(const SmallArgs& a, int fg, hipStream_t st) {
 }
 
 template <class X>
-int launch_small(const SmallArgs& a, int fg, hipStream_t st) {
-  return a.n <= 16 ? launch_small_tt<X, 1>(a, fg, st) : launch_small_tt<X, 2>(a, fg, st);
+int launch_small(const PackedCall& a, hipStream_t st) {
+  return a.n <= 16 ? launch_small_tt<X, 1>(a, st) : launch_small_tt<X, 2>(a, st);
 }
+
+// Whether the products run in tiles of many tokens.
+bool by_tiles(int64_t n) { return n > 64; }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -176,32 +165,44 @@ int cafeq_pack_nibbles(const int8_t* codes, const float* scales, int64_t out, in
   return CAFEQ_OK;
 }
 
+size_t cafeq_infer_packed_workspace_bytes(int x_type, int64_t n, int64_t out, int64_t in, int64_t group) {
+  PackedShape p;
+  if (n < 1 || x_type < CAFEQ_F32 || x_type > CAFEQ_I8 || packed_shape(out, in, group, &p) != CAFEQ_OK) return 0;
+  return by_tiles(n) ? packed_gemm_bytes(x_type, n, p) : 0;
+}
+
 int cafeq_infer_packed(const void* X, int x_type, int64_t n, int64_t ldx, const float* xscales, int64_t xgroup, const void* packed,
-                       int64_t out, int64_t in, int64_t group, void* Y, int y_dtype, int64_t ldy, void* stream) {
+                       int64_t out, int64_t in, int64_t group, void* Y, int y_dtype, int64_t ldy, void* ws, void* stream) {
   if (!X || !packed || !Y) return CAFEQ_ERR_INVALID_ARG;
   if (x_type != CAFEQ_F32 && x_type != CAFEQ_BF16 && x_type != CAFEQ_I8) return CAFEQ_ERR_INVALID_ARG;
   if (y_dtype != CAFEQ_F32 && y_dtype != CAFEQ_BF16) return CAFEQ_ERR_INVALID_ARG;
   if ((x_type == CAFEQ_I8) != (xscales != nullptr)) return CAFEQ_ERR_INVALID_ARG;
   PackedShape p;
-  int rc = packed_shape(out, in, group, &p);
+  const int rc = packed_shape(out, in, group, &p);
   if (rc) return rc;
   if (n < 0 || ldx < in || ldy < out) return CAFEQ_ERR_BAD_SHAPE;
   const int64_t gx = x_type != CAFEQ_I8 || xgroup == 0 ? in : xgroup;
   if (gx < 32 || gx % 32 != 0 || in % gx != 0) return CAFEQ_ERR_BAD_SHAPE;
-  if (n > (int64_t(1) << 20)) return CAFEQ_ERR_UNSUPPORTED;
   const int size = x_type == CAFEQ_F32 ? 4 : x_type == CAFEQ_BF16 ? 2 : 1;
+  if (n > (int64_t(1) << 20) || ldx > (int64_t(1) << 24)) return CAFEQ_ERR_UNSUPPORTED;   // a tile's offsets stay below 2^32 bytes
   if (!aligned16(X) || !aligned16(packed) || ldx * size % 16 != 0 || (reinterpret_cast<uintptr_t>(Y) & (y_dtype == CAFEQ_F32 ? 3u : 1u)) != 0 ||
       (reinterpret_cast<uintptr_t>(xscales) & 3u) != 0)
     return CAFEQ_ERR_BAD_ALIGN;
   if (n == 0) return CAFEQ_OK;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  auto step = [](int64_t g, int64_t in_) { return g == in_ || g % 128 == 0 ? 128 : g % 64 == 0 ? 64 : 32; };
-  const int fg = std::min(step(p.group, in), step(gx, in));
-  SmallArgs a{static_cast<const uint8_t*>(packed), p, X, ldx, xscales, in / gx, int((p.group + fg - 1) / fg), int((gx + fg - 1) / fg), n, Y, ldy, y_dtype};
+  auto step = [in](int64_t g) { return g == in || g % 128 == 0 ? 128 : g % 64 == 0 ? 64 : 32; };
+  const int fg = std::min(step(p.group), step(gx));
+  const PackedCall c{static_cast<const uint8_t*>(packed), p, X, x_type, n, ldx, xscales, in / gx, fg, int((p.group + fg - 1) / fg),
+                     int((gx + fg - 1) / fg), Y, ldy, y_dtype};
+  if (by_tiles(n)) {
+    if (!ws && packed_gemm_bytes(x_type, n, p)) return CAFEQ_ERR_WORKSPACE;
+    if (!aligned16(ws)) return CAFEQ_ERR_BAD_ALIGN;
+    return launch_packed_gemm(c, ws, st);
+  }
   switch (x_type) {
-    case CAFEQ_I8: return launch_small<XI8>(a, fg, st);
-    case CAFEQ_BF16: return launch_small<XBf16>(a, fg, st);
-    default: return launch_small<XF32>(a, fg, st);
+    case CAFEQ_I8: return launch_small<XI8>(c, st);
+    case CAFEQ_BF16: return launch_small<XBf16>(c, st);
+    default: return launch_small<XF32>(c, st);
   }
 }
 
