@@ -44,18 +44,33 @@ __device__ __forceinline__ void place(int id, const GemmArgs& a, int* tt, int* r
   *rt = in / size;
 }
 
+// The matrix instructions over 128 columns; lane l of an operand holds row (or token) l % 32, lane half h = l / 32
 template <bool I8> struct Form;
 template <> struct Form<true> {
-  using Acc = i32x16;
+  using Frag = i32x4;
   static constexpr int kRowBytes = 128;   // a token's 128 columns
-  static constexpr int kSteps = 4;        // matrix instructions over them
-  static __device__ __forceinline__ float value(const Acc& a, int r) { return float(a[r]); }
+  static constexpr int kSteps = 4;        // instructions: 32 columns each, half h their 16 h + 0 .. 15
+  // q0, q1: the row's chunks h and h + 2, each with 16 columns of either 64
+  static __device__ __forceinline__ void unpack(Frag (&b)[kSteps], const uint4& q0, const uint4& q1) {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const uint4& q = i & 1 ? q1 : q0;
+      const uint32_t d0 = i < 2 ? q.x : q.z, d1 = i < 2 ? q.y : q.w;
+      b[i] = i32x4{int(low16(d0)), int(high16(d0)), int(low16(d1)), int(high16(d1))};
+    }
+  }
 };
 template <> struct Form<false> {
-  using Acc = f32x16;
+  using Frag = bf16x8_t;
   static constexpr int kRowBytes = 256;
-  static constexpr int kSteps = 8;
-  static __device__ __forceinline__ float value(const Acc& a, int r) { return a[r]; }
+  static constexpr int kSteps = 8;        // 16 columns each: of block i / 2 of 32, half h its 16 h + 8 (i % 2) + 0 .. 7
+  static __device__ __forceinline__ void unpack(Frag (&b)[kSteps], const uint4& q0, const uint4& q1) {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const uint4& q = i >> 1 & 1 ? q1 : q0;
+      b[i] = bf16_codes(i < 4 ? (i & 1 ? q.y : q.x) : (i & 1 ? q.w : q.z));
+    }
+  }
 };
 
 template <bool I8, int MT, int FG, bool SX>
@@ -72,16 +87,16 @@ __global__ __launch_bounds__(kThreads, 2) void packed_gemm_kernel(const GemmArgs
   // which tile, which of its stages
   const int nkb = int(a.p.kblocks), stages = nkb * a.planes;
   int id = blockIdx.x, s0 = 0, s1 = stages, piece = -1;
-  {
-    const int total = gridDim.x;
-    if ((total & 7) == 0) id = (id & 7) * (total >> 3) + (id >> 3);   // neighbours behind one L2
-    if (id >= a.whole) {
-      piece = id - a.whole;
-      const int k = piece % a.split;
-      id = a.whole + piece / a.split;
-      s0 = int(int64_t(stages) * k / a.split);
-      s1 = int(int64_t(stages) * (k + 1) / a.split);
-    }
+  // whole tiles, and pieces, that are neighbours behind one L2 (workgroups go round the eight XCDs in turn)
+  auto near = [](int i, int total) { return (total & 7) == 0 ? (i & 7) * (total >> 3) + (i >> 3) : i; };
+  if (id < a.whole) {
+    id = near(id, a.whole);
+  } else {
+    piece = near(id - a.whole, gridDim.x - a.whole);
+    const int k = piece % a.split;
+    id = a.whole + piece / a.split;
+    s0 = int(int64_t(stages) * k / a.split);
+    s1 = int(int64_t(stages) * (k + 1) / a.split);
   }
   int tt, rt;
   place(id, a, &tt, &rt);
@@ -151,12 +166,12 @@ __global__ __launch_bounds__(kThreads, 2) void packed_gemm_kernel(const GemmArgs
   load_w(kb);
   for (int s = s0; s < s1; ++s) {
     const int slot = (s - s0) & 1;
-    uint4 w[NT][2];
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this stage's activations and weights
+    typename F::Frag b[NT][F::kSteps];
     float sc[NT][UPB];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      w[t][0] = wq[t][0];
-      w[t][1] = wq[t][1];
+      F::unpack(b[t], wq[t][0], wq[t][1]);
 #pragma unroll
       for (int u = 0; u < UPB; ++u) sc[t][u] = sw[t][u];
     }
@@ -166,7 +181,6 @@ __global__ __launch_bounds__(kThreads, 2) void packed_gemm_kernel(const GemmArgs
 #pragma unroll
         for (int u = 0; u < UPB; ++u) xs[u * TOK + tid] = sx[u];
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if constexpr (!I8) {
       // past the matrix's columns LDS holds others of the token, of which an infinity times a code of zero would be no number
@@ -185,56 +199,47 @@ __global__ __launch_bounds__(kThreads, 2) void packed_gemm_kernel(const GemmArgs
     const unsigned char* xt = smem + slot * SLOT + l31 * ROWB;
     const int sz = l31 & 7;
     if constexpr (I8) {
-      i32x4 b[NT][4];
+      // Tiles one after another, (token tile, unit, row tile).  While a tile's instructions run, the one before it is taken up in
+      // float32: from the second instruction on, when the last one's result is there.
+      constexpr int PER = NT * UPB, TILES = MT * PER;
+      i32x4 x[4];
+      i32x16 acc[2];
+      auto read_x = [&](int m, int i) __attribute__((always_inline)) {
+        x[i] = *reinterpret_cast<const i32x4*>(xt + m * 32 * ROWB + ((2 * i + h) ^ sz) * 16);
+      };
+      auto take = [&](int j, int q0, int q1) __attribute__((always_inline)) {
+        const int m = j / PER, u = j / NT % UPB, t = j % NT;
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+        for (int q = q0; q < q1; ++q) {
+          f32x4 f;
+          if constexpr (SX) f = *reinterpret_cast<const f32x4*>(xs + u * TOK + m * 32 + 8 * q + 4 * h);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint4 q = w[t][i & 1];
-          const uint32_t d0 = i < 2 ? q.x : q.z, d1 = i < 2 ? q.y : q.w;
-          b[t][i] = i32x4{int(low16(d0)), int(high16(d0)), int(low16(d1)), int(high16(d1))};
-        }
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        i32x4 x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const i32x4*>(xt + m * 32 * ROWB + ((2 * i + h) ^ sz) * 16);
-#pragma unroll
-        for (int u = 0; u < UPB; ++u) {
-          i32x16 acc[NT];
-#pragma unroll
-          for (int t = 0; t < NT; ++t) acc[t] = i32x16{};
-#pragma unroll
-          for (int i = u * SPU; i < (u + 1) * SPU; ++i)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) acc[t] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[i], b[t][i], acc[t], 0, 0, 0);
-          if constexpr (SX) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const f32x4 f = *reinterpret_cast<const f32x4*>(xs + u * TOK + m * 32 + 8 * q + 4 * h);
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) y[m][t][4 * q + e] = fmaf(float(acc[t][4 * q + e]) * f[e], sc[t][u], y[m][t][4 * q + e]);
-            }
-          } else {
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-              for (int r = 0; r < 16; ++r) y[m][t][r] = fmaf(float(acc[t][r]), sc[t][u], y[m][t][r]);
+          for (int e = 0; e < 4; ++e) {
+            const float v = float(acc[j & 1][4 * q + e]);
+            y[m][t][4 * q + e] = fmaf(SX ? v * f[e] : v, sc[t][u], y[m][t][4 * q + e]);
           }
         }
-      }
-    } else {
-      // eight instructions of 16 columns: i / 2 the block of 32; lane half h has its columns 16 h + 8 (i % 2) + 0 .. 7
-      bf16x8_t b[NT][8];
+      };
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int i = 0; i < 4; ++i) read_x(0, i);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint4 q = w[t][i >> 1 & 1];
-          b[t][i] = bf16_codes(i < 4 ? (i & 1 ? q.y : q.x) : (i & 1 ? q.w : q.z));
+      for (int j = 0; j < TILES; ++j) {
+        const int m = j / PER, u = j / NT % UPB, t = j % NT;
+#pragma unroll
+        for (int i = 0; i < SPU; ++i) {
+          acc[j & 1] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[u * SPU + i], b[t][u * SPU + i], i == 0 ? i32x16{} : acc[j & 1], 0, 0, 0);
+          if (t == NT - 1 && m + 1 < MT) read_x(m + 1, u * SPU + i);
+          __builtin_amdgcn_sched_barrier(0);
+          if (j > 0) {
+            if (SPU == 4) take(j - 1, i == 0 ? 0 : i - 1, i == 0 ? 0 : i == 3 ? 4 : i);
+            else if (SPU == 2) take(j - 1, i, i == 0 ? 1 : 4);
+            else take(j - 1, 0, 4);
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
+      }
+      take(TILES - 1, 0, 4);
+    } else {
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
