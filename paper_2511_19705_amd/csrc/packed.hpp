@@ -35,6 +35,10 @@ inline int packed_shape(int64_t out, int64_t in, int64_t group, PackedShape* p) 
   return CAFEQ_OK;
 }
 
+// The group of a unit, unit / units, by a product: units are at most 2048, where ceil(2^32 / units) is exact enough for whole quotients
+inline uint32_t unit_inverse(int units) { return units > 1 ? uint32_t(((uint64_t(1) << 32) + units - 1) / units) : 0u; }
+__device__ __forceinline__ int unit_group(int unit, int units, uint32_t inv) { return units > 1 ? int(__umulhi(uint32_t(unit), inv)) : unit; }
+
 // A checked call of cafeq_infer_packed
 struct PackedCall {
   const uint8_t* packed;
@@ -46,6 +50,7 @@ struct PackedCall {
   int64_t xgroups;
   int fg;                 // columns a unit: sums start anew there and take their scales
   int wunits, xunits;     // units a scale of the weights, of the activations
+  uint32_t winv, xinv;    // their unit_inverse()
   void* y;
   int64_t ldy;
   int ydtype;
@@ -88,49 +93,53 @@ __device__ __forceinline__ void store_y(void* y, int dtype, int64_t at, float v)
       (u & 0x7FFFFFFFu) > 0x7F800000u ? uint16_t((u >> 16) | 0x40u) : uint16_t((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16);
 }
 
-// The forms of the activations.  Chunk: 16 consecutive columns of a token (a lane's share of 64); mul: 64 columns of 16 rows times
-// 16 tokens onto acc, the weights' two dwords of the same columns.
+// The forms of the activations.  Chunk: 16 consecutive columns of a token (a lane's share of 64) as loaded; Form: as the matrix
+// instructions take them; mul: 64 columns of 16 rows times 16 tokens onto acc, the weights' two dwords of the same columns.
 struct XI8 {
   static constexpr bool kScaled = true;
+  static constexpr int kSize = 1;
   using Acc = i32x4;
-  struct Chunk { i32x4 v; };
-  static __device__ __forceinline__ Chunk load(const void* x, int64_t at, bool in) {
-    Chunk c;
-    c.v = in ? *reinterpret_cast<const i32x4*>(static_cast<const int8_t*>(x) + at) : i32x4{0, 0, 0, 0};
-    return c;
+  using Chunk = i32x4;
+  using Form = i32x4;
+  static __device__ __forceinline__ Chunk load(const void* x, int at, bool in) {
+    return in ? *reinterpret_cast<const i32x4*>(static_cast<const int8_t*>(x) + at) : i32x4{0, 0, 0, 0};
   }
-  static __device__ __forceinline__ Chunk keep(const Chunk& c, bool yes) { return yes ? c : Chunk{i32x4{0, 0, 0, 0}}; }
-  static __device__ __forceinline__ void mul(Acc& acc, uint32_t w0, uint32_t w1, const Chunk& c) {
+  static __device__ __forceinline__ void form(Form& f, const Chunk& c) { f = c; }
+  static __device__ __forceinline__ void mul(Acc& acc, uint32_t w0, uint32_t w1, const Form& f) {
     const i32x4 a = {int(low16(w0)), int(high16(w0)), int(low16(w1)), int(high16(w1))};
-    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, c.v, acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, f, acc, 0, 0, 0);
   }
   static __device__ __forceinline__ float value(const Acc& acc, int r) { return float(acc[r]); }
 };
 
 struct XBf16 {
   static constexpr bool kScaled = false;
+  static constexpr int kSize = 2;
   using Acc = f32x4;
   struct Chunk { bf16x8_t v[2]; };
-  static __device__ __forceinline__ Chunk load(const void* x, int64_t at, bool in) {
+  using Form = Chunk;
+  static __device__ __forceinline__ Chunk load(const void* x, int at, bool in) {
     Chunk c;
     const bf16x8_t* p = reinterpret_cast<const bf16x8_t*>(static_cast<const uint16_t*>(x) + at);
     c.v[0] = in ? p[0] : bf16x8_t{};
     c.v[1] = in ? p[1] : bf16x8_t{};
     return c;
   }
-  static __device__ __forceinline__ Chunk keep(const Chunk& c, bool yes) { return yes ? c : Chunk{}; }
-  static __device__ __forceinline__ void mul(Acc& acc, uint32_t w0, uint32_t w1, const Chunk& c) {
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_codes(w0), c.v[0], acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_codes(w1), c.v[1], acc, 0, 0, 0);
+  static __device__ __forceinline__ void form(Form& f, const Chunk& c) { f = c; }
+  static __device__ __forceinline__ void mul(Acc& acc, uint32_t w0, uint32_t w1, const Form& f) {
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_codes(w0), f.v[0], acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_codes(w1), f.v[1], acc, 0, 0, 0);
   }
   static __device__ __forceinline__ float value(const Acc& acc, int r) { return acc[r]; }
 };
 
 struct XF32 {
   static constexpr bool kScaled = false;
+  static constexpr int kSize = 4;
   using Acc = f32x4;
   struct Chunk { float v[16]; };
-  static __device__ __forceinline__ Chunk load(const void* x, int64_t at, bool in) {
+  struct Form { bf16x8_t v[2][3]; };   // three parts of every activation, hi + mid + lo exactly
+  static __device__ __forceinline__ Chunk load(const void* x, int at, bool in) {
     Chunk c;
     const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(x) + at);
 #pragma unroll
@@ -140,23 +149,27 @@ struct XF32 {
     }
     return c;
   }
-  static __device__ __forceinline__ Chunk keep(const Chunk& c, bool yes) { return yes ? c : Chunk{}; }
-  // three parts of every activation, hi + mid + lo exactly, the small ones first
-  static __device__ __forceinline__ void mul(Acc& acc, uint32_t w0, uint32_t w1, const Chunk& c) {
+  static __device__ __forceinline__ void form(Form& f, const Chunk& c) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      union { uint32_t u[4]; bf16x8_t v; } part[3];
       float r[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) r[i] = c.v[8 * e + i];
 #pragma unroll
-      for (int s = 0; s < 3; ++s)
+      for (int s = 0; s < 3; ++s) {
+        union { uint32_t u[4]; bf16x8_t v; } part;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) part[s].u[i] = split_pair(r[2 * i], r[2 * i + 1]);
+        for (int i = 0; i < 4; ++i) part.u[i] = split_pair(r[2 * i], r[2 * i + 1]);
+        f.v[e][s] = part.v;
+      }
+    }
+  }
+  static __device__ __forceinline__ void mul(Acc& acc, uint32_t w0, uint32_t w1, const Form& f) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
       const bf16x8_t w = bf16_codes(e ? w1 : w0);
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, part[2].v, acc, 0, 0, 0);
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, part[1].v, acc, 0, 0, 0);
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, part[0].v, acc, 0, 0, 0);
+#pragma unroll
+      for (int s = 2; s >= 0; --s) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, f.v[e][s], acc, 0, 0, 0);   // the small parts first
     }
   }
   static __device__ __forceinline__ float value(const Acc& acc, int r) { return acc[r]; }

@@ -1,6 +1,6 @@
 // Products with packed 4-bit weights for many tokens: tiles on the 32x32 matrix instructions.
 //   y[t][o] = sum over units of s[o][unit] (sx[t][unit]) sum_{c in unit} q[o][c] x[t][c]
-// A workgroup of four waves owns 32 MT tokens x 256 rows of the weight; a wave owns all its tokens and 64 of the rows.  The
+// A workgroup of four waves owns 32 MT tokens x 128 NT rows of the weight; a wave owns all its tokens and 32 NT of the rows.  The
 // activations of 128 columns go to LDS asynchronously, a stage ahead of the one being multiplied; the weights, which no other
 // wave of the workgroup needs, go to registers, 4 bits a weight, and are unpacked there once for the 32 MT tokens.
 #include "cafeq_common.hpp"
@@ -13,7 +13,7 @@ namespace {
 using i32x16 = __attribute__((__vector_size__(16 * sizeof(int)))) int;
 using f32x16 = __attribute__((__vector_size__(16 * sizeof(float)))) float;
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves, kWaveRows = 64, kTileRows = kWaves * kWaveRows;
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
 
 struct GemmArgs {
   const uint8_t* packed;
@@ -25,6 +25,7 @@ struct GemmArgs {
   const float* xscales;   // [n][xgroups]
   int64_t xgroups;
   int wunits, xunits;     // units a scale
+  uint32_t winv, xinv;
   int64_t n;
   void* y;
   int64_t ldy;
@@ -32,7 +33,7 @@ struct GemmArgs {
   int tok_tiles, row_tiles;  // tiles of the workgroups
   int whole;              // tiles that one workgroup takes whole; of the others every one goes to `split` of them
   int split;
-  float* part;            // [tile - whole][split][32 MT * 256], in the accumulators' order
+  float* part;            // [tile - whole][split][32 MT * 128 NT], in the accumulators' order
 };
 
 // tile number -> (token tile, row tile): token tiles of a group of eight side by side, so that workgroups that run together share
@@ -44,43 +45,74 @@ __device__ __forceinline__ void place(int id, const GemmArgs& a, int* tt, int* r
   *rt = in / size;
 }
 
-// The matrix instructions over 128 columns; lane l of an operand holds row (or token) l % 32, lane half h = l / 32
+// The matrix instructions over a stage's 128 columns, in kParts runs of four; lane l of an operand holds row (or token) l % 32, lane
+// half h = l / 32
 template <bool I8> struct Form;
 template <> struct Form<true> {
   using Frag = i32x4;
+  using Acc = i32x16;
   static constexpr int kRowBytes = 128;   // a token's 128 columns
-  static constexpr int kSteps = 4;        // instructions: 32 columns each, half h their 16 h + 0 .. 15
+  static constexpr int kParts = 1;        // instruction i: 32 columns, half h their 16 h + 0 .. 15
   // q0, q1: the row's chunks h and h + 2, each with 16 columns of either 64
-  static __device__ __forceinline__ void unpack(Frag (&b)[kSteps], const uint4& q0, const uint4& q1) {
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      const uint4& q = i & 1 ? q1 : q0;
-      const uint32_t d0 = i < 2 ? q.x : q.z, d1 = i < 2 ? q.y : q.w;
-      b[i] = i32x4{int(low16(d0)), int(high16(d0)), int(low16(d1)), int(high16(d1))};
-    }
+  static __device__ __forceinline__ Frag unpack(const uint4& q0, const uint4& q1, int, int i) {
+    const uint4& q = i & 1 ? q1 : q0;
+    const uint32_t d0 = i < 2 ? q.x : q.z, d1 = i < 2 ? q.y : q.w;
+    return i32x4{int(low16(d0)), int(high16(d0)), int(low16(d1)), int(high16(d1))};
   }
+  static __device__ __forceinline__ int chunk(int, int i, int h) { return 2 * i + h; }
+  static __device__ __forceinline__ Acc mul(const Frag& x, const Frag& b, const Acc& c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(x, b, c, 0, 0, 0); }
 };
 template <> struct Form<false> {
   using Frag = bf16x8_t;
+  using Acc = f32x16;
   static constexpr int kRowBytes = 256;
-  static constexpr int kSteps = 8;        // 16 columns each: of block i / 2 of 32, half h its 16 h + 8 (i % 2) + 0 .. 7
-  static __device__ __forceinline__ void unpack(Frag (&b)[kSteps], const uint4& q0, const uint4& q1) {
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      const uint4& q = i >> 1 & 1 ? q1 : q0;
-      b[i] = bf16_codes(i < 4 ? (i & 1 ? q.y : q.x) : (i & 1 ? q.w : q.z));
-    }
+  static constexpr int kParts = 2;        // instruction i of part p: of the block of 32 2 p + i / 2, half h its 16 h + 8 (i % 2) + 0 .. 7
+  static __device__ __forceinline__ Frag unpack(const uint4& q0, const uint4& q1, int p, int i) {
+    const uint4& q = i >> 1 ? q1 : q0;
+    return bf16_codes(p ? (i & 1 ? q.w : q.z) : (i & 1 ? q.y : q.x));
   }
+  static __device__ __forceinline__ int chunk(int p, int i, int h) { return 4 * (2 * p + (i >> 1)) + 2 * h + (i & 1); }
+  static __device__ __forceinline__ Acc mul(const Frag& x, const Frag& b, const Acc& c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, b, c, 0, 0, 0); }
 };
 
-template <bool I8, int MT, int FG, bool SX>
-__global__ __launch_bounds__(kThreads, 2) void packed_gemm_kernel(const GemmArgs a) {
+// What a workgroup holds in LDS: a ring of stages, as many as leave room for a second workgroup on the compute unit.  All of a stage --
+// activations, weights, scales -- is requested asynchronously, so that a wave knows how many requests follow those of a stage (weights
+// loaded to registers instead cost the compiler's waits: 3584 x 14336 and 64 tokens 28 us against 20, 1024 tokens in bfloat16 209 against 143).
+constexpr int kPerCu = 2;
+template <bool I8, int MT, int NT, int FG, bool SX>
+struct Lds {
+  static constexpr int kTok = 32 * MT, kUnits = kBlockK / FG;
+  static constexpr int kX = kTok * Form<I8>::kRowBytes;              // a stage: activations,
+  static constexpr int kW = 128 * NT * 64;                           // weights,
+  static constexpr int kSw = kWaves * kUnits * 256;                  // their scales [wave][unit][64],
+  static constexpr int kSx = SX ? kUnits * kThreads * 4 : 0;         // scales of the activations [unit][256]
+  static constexpr int kStage = kX + kW + kSw + kSx;
+  static constexpr int kRing = 80 * 1024 / kStage < 2 ? 2 : 80 * 1024 / kStage > 6 ? 6 : 80 * 1024 / kStage;
+  static constexpr int kBytes = kRing * kStage;
+  // requests of a wave for a stage
+  static constexpr int kDma = kX / 16 / kThreads + kW / 16 / kThreads + kUnits * (SX ? 2 : 1);
+};
+
+// 16 (4) bytes a lane from `src` + `off` to LDS address `to` + 16 (4) times the lane, asynchronously.  Opaque to the compiler, which would
+// otherwise drain every request before each LDS read; the addresses assume that dynamic LDS starts at 0.
+__device__ __forceinline__ void lds_dma16(uint32_t to, uint32_t off, const void* src) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(src) : "memory");
+}
+__device__ __forceinline__ void lds_dma4(uint32_t to, uint32_t off, const void* src) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(off), "s"(src) : "memory");
+}
+
+template <bool I8, int MT, int NT, int FG, bool SX>
+__global__ __launch_bounds__(kThreads, kPerCu) void packed_gemm_kernel(const GemmArgs a) {
   using F = Form<I8>;
-  constexpr int NT = 2, ROWB = F::kRowBytes, CH = ROWB / 16, SLOT = 32 * MT * ROWB;
-  constexpr int NDMA = SLOT / 16 / kThreads;        // requests of a thread and stage
-  constexpr int UPB = kBlockK / FG, SPU = F::kSteps / UPB;
+  using L = Lds<I8, MT, NT, FG, SX>;
+  constexpr int ROWB = F::kRowBytes, CH = ROWB / 16;
+  constexpr int NDMA = L::kX / 16 / kThreads;        // requests of a thread and stage
+  constexpr int UPB = kBlockK / FG;                 // units of a stage
+  constexpr int RUNS = UPB > F::kParts ? UPB / F::kParts : 1, SPU = 4 / RUNS;   // runs of SPU instructions that a part's sums are taken up after
+  constexpr int TROWS = 32 * NT * kWaves;
   constexpr int TOK = 32 * MT;
-  extern __shared__ __align__(16) unsigned char smem[];   // [2][TOK][ROWB], then [2][UPB][TOK] scales of the activations
+  extern __shared__ __align__(16) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
@@ -102,12 +134,10 @@ __global__ __launch_bounds__(kThreads, 2) void packed_gemm_kernel(const GemmArgs
   place(id, a, &tt, &rt);
   const int64_t t0 = int64_t(tt) * TOK;
   const int last = int(min(int64_t(TOK), a.n - t0)) - 1;          // last token of the tile
-  const int64_t row0 = int64_t(rt) * kTileRows + wave * kWaveRows; // the wave's first row
+  const int64_t row0 = int64_t(rt) * TROWS + wave * 32 * NT; // the wave's first row
 
   // Requests of the activations: a thread's piece i is 16 bytes of token row i * RSTEP + tid / CH (past the last one: that one's).
-  // The chunks of a token lie in LDS at their number XOR the token, so that the operand reads of eight tokens fall on distinct
-  // banks.  (Opaque to the compiler, which would otherwise drain every request before each LDS read; the address assumes
-  // that dynamic LDS starts at 0.)
+  // The chunks of a token lie in LDS at their number XOR the token, so that the operand reads of eight tokens fall on distinct banks.
   constexpr int RSTEP = kThreads / CH;
   const uint32_t ldx = uint32_t(a.ldx), rmax = uint32_t(last) * ldx, rfirst = uint32_t(tid / CH) * ldx;
   const uint32_t ch = uint32_t((tid % CH) ^ (tid / CH & 7)) * 16u;
@@ -116,40 +146,30 @@ __global__ __launch_bounds__(kThreads, 2) void packed_gemm_kernel(const GemmArgs
   auto dma = [&](int plane, int kb, int slot) __attribute__((always_inline)) {
     const uint8_t* src = xbase + plane * a.plane + int64_t(kb) * ROWB;
     const uint32_t in = kb == nkb - 1 && ch >= tail ? 0u : ch;
-    const uint32_t to = uint32_t(slot * SLOT) + uint32_t(wave) * 1024u;
+    const uint32_t to = uint32_t(slot * L::kStage) + uint32_t(wave) * 1024u;
 #pragma unroll
-    for (int i = 0; i < NDMA; ++i) {
-      const uint32_t off = min(rfirst + uint32_t(i * RSTEP) * ldx, rmax) + in;
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to + uint32_t(i) * (kThreads * 16u)), "v"(off), "s"(src)
-                   : "memory");
-    }
+    for (int i = 0; i < NDMA; ++i) lds_dma16(to + uint32_t(i) * (kThreads * 16u), min(rfirst + uint32_t(i * RSTEP) * ldx, rmax) + in, src);
   };
-  // rows past the matrix read its last tile
-  const uint4* wp[NT];
-  const float* sp[NT];
+  // the wave's scales by row; rows past the matrix read its last tile
+  const int64_t first = min(row0 / kRowTile, a.p.row_tiles - 1), srow = row0 + min(lane, 32 * NT - 1);
+  const uint32_t soff = uint32_t(((min(srow / kRowTile, a.p.row_tiles - 1) - first) * a.p.groups * kRowTile + (srow & 15)) * 4);
+  const uint8_t* sbase = a.packed + a.p.scales_at + first * a.p.groups * (kRowTile * 4);
+  auto group_w = [&](int kb, int u) { return min(unit_group(kb * UPB + u, a.wunits, a.winv), int(a.p.groups) - 1); };
+  auto group_x = [&](int kb, int u) { return min(unit_group(kb * UPB + u, a.xunits, a.xinv), int(a.xgroups) - 1); };
+  auto request = [&](int plane, int kb, int slot) __attribute__((always_inline)) {
+    dma(plane, kb, slot);
+    const uint32_t to = uint32_t(slot * L::kStage + L::kX);
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int tile = int(min(row0 / kRowTile + 2 * t + (l31 >> 4), a.p.row_tiles - 1));
-    wp[t] = reinterpret_cast<const uint4*>(a.packed) + int64_t(tile) * nkb * 64 + h * 16 + (l31 & 15);
-    sp[t] = reinterpret_cast<const float*>(a.packed + a.p.scales_at) + int64_t(tile) * a.p.groups * kRowTile + (l31 & 15);
-  }
-  uint4 wq[NT][2];
-  float sw[NT][UPB];
-  float sx[SX ? UPB : 1];
-  auto load_w = [&](int kb) __attribute__((always_inline)) {
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      wq[t][0] = wp[t][int64_t(kb) * 64];
-      wq[t][1] = wp[t][int64_t(kb) * 64 + 32];
-#pragma unroll
-      for (int u = 0; u < UPB; ++u)
-        sw[t][u] = sp[t][min((kb * UPB + u) / a.wunits, int(a.p.groups) - 1) * kRowTile];
+    for (int i = 0; i < 2 * NT; ++i) {       // the workgroup's tiles of 16 rows 4 i + wave, as they lie in memory
+      const int64_t tile = min(int64_t(rt) * (TROWS / kRowTile) + 4 * i + wave, a.p.row_tiles - 1);
+      lds_dma16(to + uint32_t(4 * i + wave) * 1024u, uint32_t(lane) * 16u, a.packed + (tile * nkb + kb) * 1024);
     }
-    if constexpr (SX) {
-      if (tid < TOK)
 #pragma unroll
-        for (int u = 0; u < UPB; ++u)
-          sx[u] = a.xscales[(t0 + min(tid, last)) * a.xgroups + min((kb * UPB + u) / a.xunits, int(a.xgroups) - 1)];
+    for (int u = 0; u < UPB; ++u) {
+      lds_dma4(to + L::kW + uint32_t(wave * UPB + u) * 256u, soff, sbase + group_w(kb, u) * (kRowTile * 4));
+      if constexpr (SX)
+        lds_dma4(to + L::kW + L::kSw + uint32_t(u * kThreads + wave * 64) * 4u, uint32_t(min(tid, last)) * uint32_t(a.xgroups * 4),
+                 a.xscales + t0 * a.xgroups + group_x(kb, u));
     }
   };
 
@@ -161,62 +181,73 @@ __global__ __launch_bounds__(kThreads, 2) void packed_gemm_kernel(const GemmArgs
 #pragma unroll
       for (int r = 0; r < 16; ++r) y[m][t][r] = 0.f;
 
-  int plane = s0 / nkb, kb = s0 % nkb;
-  dma(plane, kb, 0);
-  load_w(kb);
+  constexpr int AHEAD = L::kRing - 1;
+  int plane = s0 / nkb, kb = s0 % nkb, slot = 0;     // of the stage that is multiplied
+  int rplane = plane, rkb = kb, rslot = 0;           // of the one that is requested next (past the last one: the last one again)
+  auto request_next = [&]() __attribute__((always_inline)) {
+    request(rplane, rkb, rslot);
+    rslot = rslot + 1 == L::kRing ? 0 : rslot + 1;
+    if (rplane * nkb + rkb + 1 < s1 && ++rkb == nkb) { rkb = 0; ++rplane; }
+  };
+  for (int i = 0; i < AHEAD; ++i) request_next();
   for (int s = s0; s < s1; ++s) {
-    const int slot = (s - s0) & 1;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this stage's activations and weights
-    typename F::Frag b[NT][F::kSteps];
-    float sc[NT][UPB];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      F::unpack(b[t], wq[t][0], wq[t][1]);
-#pragma unroll
-      for (int u = 0; u < UPB; ++u) sc[t][u] = sw[t][u];
-    }
-    float* xs = reinterpret_cast<float*>(smem + 2 * SLOT) + slot * UPB * TOK;
-    if constexpr (SX) {
-      if (tid < TOK)
-#pragma unroll
-        for (int u = 0; u < UPB; ++u) xs[u * TOK + tid] = sx[u];
-    }
+    // this stage's requests: all but those of the stages after it
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 1) * L::kDma) : "memory");
     __syncthreads();
     if constexpr (!I8) {
       // past the matrix's columns LDS holds others of the token, of which an infinity times a code of zero would be no number
       if (kb == nkb - 1 && tail < uint32_t(ROWB)) {
         if (ch >= tail)
 #pragma unroll
-          for (int i = 0; i < NDMA; ++i) *reinterpret_cast<uint4*>(smem + slot * SLOT + (i * kThreads + tid) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          for (int i = 0; i < NDMA; ++i) *reinterpret_cast<uint4*>(smem + slot * L::kStage + (i * kThreads + tid) * 16) = make_uint4(0u, 0u, 0u, 0u);
         __syncthreads();
       }
     }
+    request_next();
     if (++kb == nkb) { kb = 0; ++plane; }
-    if (s + 1 < s1) {
-      dma(plane, kb, slot ^ 1);
-      load_w(kb);
+    const unsigned char* wt = smem + slot * L::kStage + L::kX;
+    const float* xs = reinterpret_cast<const float*>(wt + L::kW + L::kSw);
+    typename F::Frag b[NT][4];
+    float sc[NT][UPB];
+    uint4 w[NT][2];                                  // the lane's chunks h and h + 2 of a row
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const unsigned char* at = wt + ((wave * NT + t) * 2 + (l31 >> 4)) * 1024 + (h * 16 + (l31 & 15)) * 16;
+      w[t][0] = *reinterpret_cast<const uint4*>(at);
+      w[t][1] = *reinterpret_cast<const uint4*>(at + 512);
+#pragma unroll
+      for (int u = 0; u < UPB; ++u) sc[t][u] = *reinterpret_cast<const float*>(wt + L::kW + (wave * UPB + u) * 256 + (t * 32 + l31) * 4);
     }
-    const unsigned char* xt = smem + slot * SLOT + l31 * ROWB;
+    auto unpack = [&](int part) __attribute__((always_inline)) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b[t][i] = F::unpack(w[t][0], w[t][1], part, i);
+    };
+    const unsigned char* xt = smem + slot * L::kStage + l31 * ROWB;
     const int sz = l31 & 7;
-    if constexpr (I8) {
-      // Tiles one after another, (token tile, unit, row tile).  While a tile's instructions run, the one before it is taken up in
-      // float32: from the second instruction on, when the last one's result is there.
-      constexpr int PER = NT * UPB, TILES = MT * PER;
-      i32x4 x[4];
-      i32x16 acc[2];
+    slot = slot + 1 == L::kRing ? 0 : slot + 1;
+    // Tiles one after another, (token tile, run, row tile).  While a tile's instructions run, the one before it is taken up in
+    // float32: from the second instruction on, when the last one's result is there.
+    constexpr int PER = NT * RUNS, TILES = MT * PER;
+#pragma unroll
+    for (int part = 0; part < F::kParts; ++part) {
+      unpack(part);
+      typename F::Frag x[4];
+      typename F::Acc acc[2];
       auto read_x = [&](int m, int i) __attribute__((always_inline)) {
-        x[i] = *reinterpret_cast<const i32x4*>(xt + m * 32 * ROWB + ((2 * i + h) ^ sz) * 16);
+        x[i] = *reinterpret_cast<const typename F::Frag*>(xt + m * 32 * ROWB + (F::chunk(part, i, h) ^ sz) * 16);
       };
       auto take = [&](int j, int q0, int q1) __attribute__((always_inline)) {
-        const int m = j / PER, u = j / NT % UPB, t = j % NT;
+        const int m = j / PER, u = UPB > 1 ? part * UPB / F::kParts + j / NT % RUNS : 0, t = j % NT;
 #pragma unroll
-        for (int q = q0; q < q1; ++q) {
+        for (int v = q0; v < q1; ++v) {
           f32x4 f;
-          if constexpr (SX) f = *reinterpret_cast<const f32x4*>(xs + u * TOK + m * 32 + 8 * q + 4 * h);
+          if constexpr (SX) f = *reinterpret_cast<const f32x4*>(xs + u * kThreads + m * 32 + 8 * v + 4 * h);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float v = float(acc[j & 1][4 * q + e]);
-            y[m][t][4 * q + e] = fmaf(SX ? v * f[e] : v, sc[t][u], y[m][t][4 * q + e]);
+            const float z = float(acc[j & 1][4 * v + e]);
+            y[m][t][4 * v + e] = fmaf(SX ? z * f[e] : z, sc[t][u], y[m][t][4 * v + e]);
           }
         }
       };
@@ -224,10 +255,10 @@ __global__ __launch_bounds__(kThreads, 2) void packed_gemm_kernel(const GemmArgs
       for (int i = 0; i < 4; ++i) read_x(0, i);
 #pragma unroll
       for (int j = 0; j < TILES; ++j) {
-        const int m = j / PER, u = j / NT % UPB, t = j % NT;
+        const int m = j / PER, u = j / NT % RUNS, t = j % NT;
 #pragma unroll
         for (int i = 0; i < SPU; ++i) {
-          acc[j & 1] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[u * SPU + i], b[t][u * SPU + i], i == 0 ? i32x16{} : acc[j & 1], 0, 0, 0);
+          acc[j & 1] = F::mul(x[u * SPU + i], b[t][u * SPU + i], i == 0 ? typename F::Acc{} : acc[j & 1]);
           if (t == NT - 1 && m + 1 < MT) read_x(m + 1, u * SPU + i);
           __builtin_amdgcn_sched_barrier(0);
           if (j > 0) {
@@ -239,30 +270,12 @@ __global__ __launch_bounds__(kThreads, 2) void packed_gemm_kernel(const GemmArgs
         }
       }
       take(TILES - 1, 0, 4);
-    } else {
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int u = 0; u < UPB; ++u) {
-          f32x16 acc[NT];
-#pragma unroll
-          for (int t = 0; t < NT; ++t) acc[t] = f32x16{};
-#pragma unroll
-          for (int i = u * SPU; i < (u + 1) * SPU; ++i) {
-            const bf16x8_t x = *reinterpret_cast<const bf16x8_t*>(xt + m * 32 * ROWB + ((4 * (i >> 1) + 2 * h + (i & 1)) ^ sz) * 16);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, b[t][i], acc[t], 0, 0, 0);
-          }
-#pragma unroll
-          for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) y[m][t][r] = fmaf(acc[t][r], sc[t][u], y[m][t][r]);
-        }
     }
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // requests past the last stage
 
   if (piece >= 0) {
-    float* out = a.part + int64_t(piece) * (TOK * kTileRows) + wave * (MT * NT * 16 * 64) + lane;
+    float* out = a.part + int64_t(piece) * (TOK * TROWS) + wave * (MT * NT * 16 * 64) + lane;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -286,19 +299,18 @@ __global__ __launch_bounds__(kThreads, 2) void packed_gemm_kernel(const GemmArgs
 }
 
 // the pieces of a tile in order, to Y
-template <int MT>
-__global__ __launch_bounds__(256) void packed_join_kernel(const GemmArgs a, bool per_token) {
-  constexpr int N = 32 * MT * kTileRows, NT = 2;
+__global__ __launch_bounds__(256) void packed_join_kernel(const GemmArgs a, int mt, int nt, bool per_token) {
+  const int size = 32 * mt * 32 * nt * kWaves;
   const int tile = blockIdx.y, e = blockIdx.x * 256 + threadIdx.x;
   int tt, rt;
   place(a.whole + tile, a, &tt, &rt);
-  const int lane = e & 63, r = e >> 6 & 15, t = e >> 10 & (NT - 1), m = (e >> 11) % MT, wave = (e >> 11) / MT;
-  const int64_t tok = int64_t(tt) * 32 * MT + m * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-  const int64_t row = int64_t(rt) * kTileRows + wave * kWaveRows + t * 32 + (lane & 31);
+  const int lane = e & 63, r = e >> 6 & 15, at = e >> 10, t = at % nt, m = at / nt % mt, wave = at / nt / mt;   // as the kernel leaves them
+  const int64_t tok = int64_t(tt) * 32 * mt + m * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+  const int64_t row = int64_t(rt) * (32 * nt * kWaves) + (wave * nt + t) * 32 + (lane & 31);
   if (tok >= a.n || row >= a.p.rows) return;
-  const float* p = a.part + int64_t(tile) * a.split * N + e;
+  const float* p = a.part + int64_t(tile) * a.split * size + e;
   float v = 0.f;
-  for (int k = 0; k < a.split; ++k) v += p[int64_t(k) * N];
+  for (int k = 0; k < a.split; ++k) v += p[int64_t(k) * size];
   store_y(a.y, a.ydtype, tok * a.ldy + row, v * ((per_token ? a.xscales[tok] : 1.f) * 0.0625f));
 }
 
@@ -319,47 +331,74 @@ __global__ __launch_bounds__(256) void split_planes_of_x_kernel(const float* __r
 }
 
 struct Plan {
-  int mt, tok_tiles, row_tiles, whole, split;
-  size_t planes_at, part_at, bytes;
+  int mt, nt, tok_tiles, row_tiles, whole, split;
+  size_t part_at, bytes;
 };
 
+// What a stage of a tile takes, in us: on a compute unit alone, and with a second workgroup there (groups of 128; 4608 columns, 128 to 1024
+// workgroups).
+struct TileCost { int mt, nt; float alone, paired; };
+constexpr TileCost kTilesI8[] = {{1, 1, 0.54f, 0.71f}, {2, 1, 0.76f, 1.03f}, {2, 2, 1.25f, 2.0f}, {4, 2, 2.15f, 3.4f}};
+constexpr TileCost kTilesBf16[] = {{1, 1, 0.75f, 0.98f}, {2, 1, 0.98f, 1.42f}, {2, 2, 1.56f, 2.85f}};   // 4 x 2 leaves no room for a second workgroup: 5.0
+
+// The tile and the split with the least estimated time.  Tiles that fill rounds of workgroups run whole; of the rest every one is split along
+// the columns, as far as that fills the compute units and its partial sums (written, read, a launch more) cost less than it gains.
+// 3584 x 14336, 32 tokens of 8 bits, split 1 / 4 / 9 / 18: 60 / 21 / 16 / 18 us; 36864 x 4608 1 / 2 / 4: 26 / 33 / 34.
 Plan make_plan(int x_type, int64_t n, const PackedShape& p) {
-  Plan g{};
-  const int slots = 2 * device_cu_count();          // two workgroups a compute unit
-  g.mt = 4;
-  g.tok_tiles = int((n + 32 * g.mt - 1) / (32 * g.mt));
-  g.row_tiles = int((p.rows + kTileRows - 1) / kTileRows);
-  const int tiles = g.tok_tiles * g.row_tiles;
-  g.whole = tiles / slots * slots;
-  const int rest = tiles - g.whole;
+  Plan best{};
+  double least = 1e30;
+  const int cus = device_cu_count(), slots = kPerCu * cus;
   const int stages = int(p.kblocks) * (x_type == CAFEQ_F32 ? 3 : 1);
-  g.split = rest == 0 ? 1 : std::max(1, std::min(slots / rest, stages / 8));
-  if (g.split == 1) g.whole = tiles;
-  g.planes_at = 0;
-  g.part_at = x_type == CAFEQ_F32 ? align_up(size_t(n) * size_t(p.cols) * 6, 256) : 0;
-  g.bytes = g.part_at + size_t(tiles - g.whole) * g.split * 32 * g.mt * kTileRows * sizeof(float);
-  return g;
-}
-
-template <bool I8, int MT, int FG>
-void launch_fg(const GemmArgs& a, bool sx, unsigned nwg, hipStream_t st) {
-  constexpr size_t lds = 2 * 32 * MT * Form<I8>::kRowBytes;
-  if constexpr (I8) {
-    if (sx) {
-      hipLaunchKernelGGL((packed_gemm_kernel<I8, MT, FG, true>), dim3(nwg), dim3(kThreads), lds + 2 * (kBlockK / FG) * 32 * MT * 4, st, a);
-      return;
+  auto consider = [&](const TileCost& c) {
+    const int trows = 32 * c.nt * kWaves;
+    const int64_t tok_tiles = (n + 32 * c.mt - 1) / (32 * c.mt), row_tiles = (p.rows + trows - 1) / trows, tiles = tok_tiles * row_tiles;
+    const int64_t whole = tiles / slots * slots, rest = tiles - whole;
+    // pieces of so many stages, two workgroups a compute unit at a time; 1.5 us to begin and end one
+    auto run = [&](int64_t pieces, int64_t depth) {
+      const int64_t left = pieces % slots;
+      return double(pieces / slots) * (double(depth) * c.paired + 1.5) + (left ? double(depth) * (left > cus ? c.paired : c.alone) + 1.5 : 0.0);
+    };
+    for (int64_t split = 1; split == 1 || (split <= stages / 2 && rest * split <= 4 * slots); ++split) {
+      const double per = run(whole, stages) + run(rest * split, (stages + split - 1) / split);
+      const double join = split == 1 ? 0.0 : 4.0 + double(rest * split) * (32 * c.mt * trows * 4) * 2 / 4.5e6;
+      const double t = per + join;
+      if (t < least) {
+        least = t;
+        best.mt = c.mt; best.nt = c.nt; best.tok_tiles = int(tok_tiles); best.row_tiles = int(row_tiles);
+        best.split = int(split); best.whole = int(split == 1 ? tiles : whole);
+        best.bytes = split == 1 ? 0 : size_t(rest * split) * (32 * c.mt * trows * 4);
+      }
+      if (rest == 0) break;
     }
-  }
-  hipLaunchKernelGGL((packed_gemm_kernel<I8, MT, FG, false>), dim3(nwg), dim3(kThreads), lds, st, a);
+  };
+  if (x_type == CAFEQ_I8) for (const TileCost& c : kTilesI8) consider(c);
+  else for (const TileCost& c : kTilesBf16) consider(c);
+  best.part_at = x_type == CAFEQ_F32 ? align_up(size_t(n) * size_t(p.cols) * 6, 256) : 0;
+  best.bytes += best.part_at;
+  return best;
 }
 
-template <bool I8, int MT>
-void launch_mt(const GemmArgs& a, int fg, bool sx, unsigned nwg, hipStream_t st) {
-  switch (fg) {
-    case 128: launch_fg<I8, MT, 128>(a, sx, nwg, st); break;
-    case 64: launch_fg<I8, MT, 64>(a, sx, nwg, st); break;
-    default: launch_fg<I8, MT, 32>(a, sx, nwg, st); break;
+template <bool I8, int MT, int NT, int FG, bool SX>
+int launch_one(const GemmArgs& a, unsigned nwg, hipStream_t st) {
+  constexpr int lds = Lds<I8, MT, NT, FG, SX>::kBytes;
+  auto* kern = packed_gemm_kernel<I8, MT, NT, FG, SX>;
+  if constexpr (lds > 64 * 1024) {
+    static const bool ok = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
+    if (!ok) return CAFEQ_ERR_LAUNCH;
   }
+  hipLaunchKernelGGL(kern, dim3(nwg), dim3(kThreads), lds, st, a);
+  CAFEQ_CHECK_LAUNCH();
+  return CAFEQ_OK;
+}
+
+template <bool I8, int MT, int NT>
+int launch_tile(const GemmArgs& a, int fg, bool sx, unsigned nwg, hipStream_t st) {
+  if constexpr (I8) {
+    if (sx) return fg == 128 ? launch_one<I8, MT, NT, 128, true>(a, nwg, st) : fg == 64 ? launch_one<I8, MT, NT, 64, true>(a, nwg, st)
+                                                                                        : launch_one<I8, MT, NT, 32, true>(a, nwg, st);
+  }
+  return fg == 128 ? launch_one<I8, MT, NT, 128, false>(a, nwg, st) : fg == 64 ? launch_one<I8, MT, NT, 64, false>(a, nwg, st)
+                                                                               : launch_one<I8, MT, NT, 32, false>(a, nwg, st);
 }
 
 }  // namespace
@@ -370,12 +409,12 @@ int launch_packed_gemm(const PackedCall& c, void* ws, hipStream_t st) {
   const Plan g = make_plan(c.x_type, c.n, c.p);
   GemmArgs a{};
   a.packed = c.packed; a.p = c.p; a.n = c.n; a.y = c.y; a.ldy = c.ldy; a.ydtype = c.ydtype;
-  a.xscales = c.xscales; a.xgroups = c.xgroups; a.wunits = c.wunits; a.xunits = c.xunits;
+  a.xscales = c.xscales; a.xgroups = c.xgroups; a.wunits = c.wunits; a.xunits = c.xunits; a.winv = c.winv; a.xinv = c.xinv;
   a.planes = 1;
   a.x = static_cast<const uint8_t*>(c.x);
   a.ldx = c.ldx * (c.x_type == CAFEQ_I8 ? 1 : 2);
   if (c.x_type == CAFEQ_F32) {
-    uint16_t* planes = reinterpret_cast<uint16_t*>(static_cast<char*>(ws) + g.planes_at);
+    uint16_t* planes = static_cast<uint16_t*>(ws);
     const int64_t pieces = c.n * (c.p.cols / 8);
     hipLaunchKernelGGL(split_planes_of_x_kernel, dim3(unsigned((pieces + 255) / 256)), dim3(256), 0, st, static_cast<const float*>(c.x), c.ldx, c.n,
                        c.p.cols, planes);
@@ -389,13 +428,18 @@ int launch_packed_gemm(const PackedCall& c, void* ws, hipStream_t st) {
   a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + g.part_at);
   const int rest = g.tok_tiles * g.row_tiles - g.whole;
   const unsigned nwg = unsigned(g.whole + rest * g.split);
-  const bool sx = c.x_type == CAFEQ_I8 && c.xgroups > 1;
-  if (c.x_type == CAFEQ_I8) launch_mt<true, 4>(a, c.fg, sx, nwg, st);
-  else launch_mt<false, 4>(a, c.fg, false, nwg, st);
-  CAFEQ_CHECK_LAUNCH();
+  const bool i8 = c.x_type == CAFEQ_I8, sx = i8 && c.xgroups > 1;
+  int rc = CAFEQ_ERR_UNSUPPORTED;
+  switch (g.mt * 10 + g.nt) {
+    case 11: rc = i8 ? launch_tile<true, 1, 1>(a, c.fg, sx, nwg, st) : launch_tile<false, 1, 1>(a, c.fg, false, nwg, st); break;
+    case 21: rc = i8 ? launch_tile<true, 2, 1>(a, c.fg, sx, nwg, st) : launch_tile<false, 2, 1>(a, c.fg, false, nwg, st); break;
+    case 22: rc = i8 ? launch_tile<true, 2, 2>(a, c.fg, sx, nwg, st) : launch_tile<false, 2, 2>(a, c.fg, false, nwg, st); break;
+    case 42: rc = launch_tile<true, 4, 2>(a, c.fg, sx, nwg, st); break;
+  }
+  if (rc) return rc;
   if (rest) {
-    const bool per_token = c.x_type == CAFEQ_I8 && !sx;
-    hipLaunchKernelGGL(packed_join_kernel<4>, dim3(32 * 4 * kTileRows / 256, rest), dim3(256), 0, st, a, per_token);
+    const int size = 32 * g.mt * 32 * g.nt * kWaves;
+    hipLaunchKernelGGL(packed_join_kernel, dim3(size / 256, rest), dim3(256), 0, st, a, g.mt, g.nt, i8 && !sx);
     CAFEQ_CHECK_LAUNCH();
   }
   return CAFEQ_OK;

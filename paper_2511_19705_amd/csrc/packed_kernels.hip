@@ -41,102 +41,169 @@ __global__ __launch_bounds__(256) void pack_kernel(const int8_t* __restrict__ co
   }
 }
 
-// A workgroup owns 16 rows of the weight and 16 TT tokens; its waves share the columns, 128 at a time, and add up through LDS.
-// v_mfma 16x16: A the codes (16 rows), B the activations (16 tokens): a lane has four rows of one token, whose scales are one
-// 16-byte load.  Sums start anew every FG columns (the common divisor of both groups and 128) and are taken up in float32 with
-// their scales.
-template <class X, int TT, int FG>
+// A workgroup owns 16 OT rows of the weight and 16 TT tokens; its waves share the columns, each a run of blocks of 128, and add up
+// through LDS in order.  v_mfma 16x16: A the codes (16 rows), B the activations (16 tokens): a lane has four rows of one token, whose
+// scales are one 16-byte load.  Sums start anew every FG columns (the common divisor of both groups and 128) and are taken up in
+// float32 with their scales.  A wave requests U blocks at once (weights, activations, scales) before it multiplies the first: with few
+// tokens nothing but the bytes in flight counts.
+template <class X, int TT, int OT, int FG>
 __global__ __launch_bounds__(1024) void packed_small_kernel(const PackedCall a) {
   extern __shared__ float red[];
+  constexpr int UPB = kBlockK / FG;                 // units of a block
+  constexpr int U = TT * OT > 1 || FG == 32 ? 1 : 2;   // blocks requested at once
   const int tid = threadIdx.x, lane = tid & 63, nwave = blockDim.x >> 6;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, kq = lane >> 4;
-  const int64_t rt = blockIdx.x, t0 = int64_t(blockIdx.y) * 16 * TT;
+  const int rt0 = blockIdx.x * OT, t0 = blockIdx.y * 16 * TT;
   const int nkb = int(a.p.kblocks), kb0 = wave * nkb / nwave, kb1 = (wave + 1) * nkb / nwave;
-  const uint4* w = reinterpret_cast<const uint4*>(a.packed) + (rt * nkb) * 64 + lane;
-  const float* sw = reinterpret_cast<const float*>(a.packed + a.p.scales_at) + rt * a.p.groups * kRowTile + kq * 4;
-  f32x4 y[TT];
+  const int cols = int(a.p.cols), ngroup = int(a.p.groups), nxgroup = int(a.xgroups);
+  const uint4* w[OT];
+  const float* sw[OT];
 #pragma unroll
-  for (int tt = 0; tt < TT; ++tt) y[tt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  constexpr int UPB = kBlockK / FG;                 // units a block of 128 columns
-  int wu = kb0 * UPB % a.wunits, wg = kb0 * UPB / a.wunits;
-  int xu = X::kScaled ? kb0 * UPB % a.xunits : 0, xg = X::kScaled ? kb0 * UPB / a.xunits : 0;
-  for (int kb = kb0; kb < kb1; ++kb) {
-    const uint4 q = w[int64_t(kb) * 64];
-    const uint32_t qd[4] = {q.x, q.y, q.z, q.w};
-    typename X::Chunk xv[TT][2];
+  for (int o = 0; o < OT; ++o) {
+    const int64_t rt = min(rt0 + o, int(a.p.row_tiles) - 1);
+    w[o] = reinterpret_cast<const uint4*>(a.packed) + rt * nkb * 64 + lane;
+    sw[o] = reinterpret_cast<const float*>(a.packed + a.p.scales_at) + rt * ngroup * kRowTile + kq * 4;
+  }
+  const void* xp[TT];
+  const float* sxp[TT];
+  bool live[TT];
 #pragma unroll
-    for (int tt = 0; tt < TT; ++tt) {
-      const int64_t t = t0 + tt * 16 + l16;
+  for (int t = 0; t < TT; ++t) {
+    const int64_t tok = t0 + 16 * t + l16;
+    live[t] = tok < a.n;
+    xp[t] = static_cast<const char*>(a.x) + (live[t] ? tok : 0) * a.ldx * X::kSize;
+    sxp[t] = X::kScaled ? a.xscales + (live[t] ? tok : 0) * a.xgroups : nullptr;
+  }
+  f32x4 y[OT][TT];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int64_t k = int64_t(kb) * kBlockK + 64 * j + 16 * kq;
-        xv[tt][j] = X::load(a.x, t * a.ldx + k, t < a.n && k < a.p.cols);
+  for (int o = 0; o < OT; ++o)
+#pragma unroll
+    for (int t = 0; t < TT; ++t) y[o][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int kb = kb0; kb < kb1; kb += U) {
+    uint4 q[U][OT];
+    typename X::Chunk xv[U][TT][2];
+    f32x4 s4[U][UPB][OT];
+    float sx[U][UPB][TT];
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (kb + i < kb1) {
+#pragma unroll
+        for (int o = 0; o < OT; ++o) q[i][o] = w[o][(kb + i) * 64];
       }
-    }
 #pragma unroll
-    for (int u = 0; u < UPB; ++u) {
-      const f32x4 s4 = *reinterpret_cast<const f32x4*>(sw + int64_t(min(wg, int(a.p.groups) - 1)) * kRowTile);
+    for (int i = 0; i < U; ++i)
+      if (kb + i < kb1) {
 #pragma unroll
-      for (int tt = 0; tt < TT; ++tt) {
-        typename X::Acc acc = {};
-        if constexpr (FG == 128) {
-          X::mul(acc, qd[0], qd[1], xv[tt][0]);
-          X::mul(acc, qd[2], qd[3], xv[tt][1]);
-        } else if constexpr (FG == 64) {
-          X::mul(acc, qd[2 * u], qd[2 * u + 1], xv[tt][u]);
-        } else {
-          // 32 of the 64 columns: the other lanes' activations as zeros
-          X::mul(acc, qd[2 * (u >> 1)], qd[2 * (u >> 1) + 1], X::keep(xv[tt][u >> 1], (kq >> 1) == (u & 1)));
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int k = (kb + i) * kBlockK + 64 * j + 16 * kq;
+            xv[i][t][j] = X::load(xp[t], k, live[t] && k < cols);
+          }
+#pragma unroll
+        for (int u = 0; u < UPB; ++u) {
+          const int unit = (kb + i) * UPB + u;
+          const int wg = min(unit_group(unit, a.wunits, a.winv), ngroup - 1);
+#pragma unroll
+          for (int o = 0; o < OT; ++o) s4[i][u][o] = *reinterpret_cast<const f32x4*>(sw[o] + wg * kRowTile);
+          if constexpr (X::kScaled) {
+            const int xg = min(unit_group(unit, a.xunits, a.xinv), nxgroup - 1);
+#pragma unroll
+            for (int t = 0; t < TT; ++t) sx[i][u][t] = sxp[t][xg];
+          }
         }
-        float sx = 1.f;
-        if constexpr (X::kScaled) {
-          const int64_t t = t0 + tt * 16 + l16;
-          sx = t < a.n ? a.xscales[t * a.xgroups + min(xg, int(a.xgroups) - 1)] : 0.f;
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) y[tt][r] = fmaf(X::value(acc, r) * sx, s4[r], y[tt][r]);
       }
-      if (++wu == a.wunits) { wu = 0; ++wg; }
-      if constexpr (X::kScaled) if (++xu == a.xunits) { xu = 0; ++xg; }
-    }
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (kb + i < kb1) {
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+          typename X::Form xf[2];
+          X::form(xf[0], xv[i][t][0]);
+          X::form(xf[1], xv[i][t][1]);
+#pragma unroll
+          for (int o = 0; o < OT; ++o) {
+            const uint4& c = q[i][o];
+#pragma unroll
+            for (int u = 0; u < UPB; ++u) {
+              typename X::Acc acc = {};
+              if constexpr (FG == 128) {
+                X::mul(acc, c.x, c.y, xf[0]);
+                X::mul(acc, c.z, c.w, xf[1]);
+              } else if constexpr (FG == 64) {
+                X::mul(acc, u ? c.z : c.x, u ? c.w : c.y, xf[u]);
+              } else {
+                // 32 of 64 columns: the codes of the other lanes as zeros
+                const uint32_t keep = (kq >> 1) == (u & 1) ? 0xFFFFFFFFu : 0u;
+                X::mul(acc, (u >> 1 ? c.z : c.x) & keep, (u >> 1 ? c.w : c.y) & keep, xf[u >> 1]);
+              }
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                float v = X::value(acc, r);
+                if constexpr (X::kScaled) v *= sx[i][u][t];
+                y[o][t][r] = fmaf(v, s4[i][u][o][r], y[o][t][r]);
+              }
+            }
+          }
+        }
+      }
   }
 #pragma unroll
-  for (int tt = 0; tt < TT; ++tt) *reinterpret_cast<f32x4*>(&red[((wave * TT + tt) * 64 + lane) * 4]) = y[tt];
+  for (int o = 0; o < OT; ++o)
+#pragma unroll
+    for (int t = 0; t < TT; ++t) *reinterpret_cast<f32x4*>(&red[(((wave * OT + o) * TT + t) * 64 + lane) * 4]) = y[o][t];
   __syncthreads();
-  // value e: token e / 16, row e % 16
-  for (int e = tid; e < 256 * TT; e += blockDim.x) {
-    const int o = e & 15, tok = e >> 4;
-    const int64_t t = t0 + tok, row = rt * kRowTile + o;
-    const int at = (((tok >> 4) * 64) + (o >> 2) * 16 + (tok & 15)) * 4 + (o & 3);
+  // value e: token e / (16 OT), row e % (16 OT)
+  for (int e = tid; e < 256 * OT * TT; e += blockDim.x) {
+    const int o = e & 15, ot = (e >> 4) % OT, tok = (e >> 4) / OT;
+    const int at = ((ot * TT + (tok >> 4)) * 64 + (o >> 2) * 16 + (tok & 15)) * 4 + (o & 3);
+    const int64_t row = int64_t(rt0 + ot) * kRowTile + o;
     float v = 0.f;
-    for (int i = 0; i < nwave; ++i) v += red[i * TT * 256 + at];
-    if (t < a.n && row < a.p.rows) store_y(a.y, a.ydtype, t * a.ldy + row, v * 0.0625f);
+    for (int i = 0; i < nwave; ++i) v += red[i * OT * TT * 256 + at];
+    if (t0 + tok < a.n && row < a.p.rows) store_y(a.y, a.ydtype, (t0 + tok) * a.ldy + row, v * 0.0625f);
   }
 }
 
-template <class X, int TT>
+template <class X, int TT, int OT>
 int launch_small_tt(const PackedCall& a, hipStream_t st) {
-  const int64_t nkb = a.p.kblocks;
-  const int nw = int(std::min<int64_t>(16, std::max<int64_t>(1, nkb / 2)));
-  const dim3 grid(unsigned((a.p.rows + kRowTile - 1) / kRowTile), unsigned((a.n + 16 * TT - 1) / (16 * TT)));
-  const size_t lds = size_t(nw) * TT * 1024;
+  const int nkb = int(a.p.kblocks);
+  const unsigned gx = unsigned((a.p.rows + kRowTile * OT - 1) / (kRowTile * OT)), gy = unsigned((a.n + 16 * TT - 1) / (16 * TT));
+  // Sixteen waves a compute unit; no more of them to a workgroup than that takes (36864 x 4608, one token, 16 / 4 waves: 23 / 16.5 us), as many
+  // where rows are few (3584 x 14336, 4 / 16: 9.7 / 7.6)
+  int nw = 16 / OT;
+  while (nw > 1 && (int64_t(gx) * gy * (nw / 2) >= 16 * device_cu_count() || nkb < nw * 2)) nw /= 2;
+  const dim3 grid(gx, gy);
+  const size_t lds = size_t(nw) * OT * TT * 1024;
   switch (a.fg) {
-    case 128: hipLaunchKernelGGL((packed_small_kernel<X, TT, 128>), grid, dim3(nw * 64), lds, st, a); break;
-    case 64: hipLaunchKernelGGL((packed_small_kernel<X, TT, 64>), grid, dim3(nw * 64), lds, st, a); break;
-    default: hipLaunchKernelGGL((packed_small_kernel<X, TT, 32>), grid, dim3(nw * 64), lds, st, a); break;
+    case 128: hipLaunchKernelGGL((packed_small_kernel<X, TT, OT, 128>), grid, dim3(nw * 64), lds, st, a); break;
+    case 64: hipLaunchKernelGGL((packed_small_kernel<X, TT, OT, 64>), grid, dim3(nw * 64), lds, st, a); break;
+    default: hipLaunchKernelGGL((packed_small_kernel<X, TT, OT, 32>), grid, dim3(nw * 64), lds, st, a); break;
   }
   CAFEQ_CHECK_LAUNCH();
   return CAFEQ_OK;
 }
 
-template <class X>
+// Two row tiles a wave share its activations, whose way from L2 then weighs less (8 bits, 36864 x 4608, 16 tokens: 30 -> 23.5 us), where the
+// workgroups still fill the chip (3584 x 14336: 13.6 -> 17); float activations of two row or token tiles leave too few registers
+// (bfloat16, 36864 x 4608, 8 tokens: 31 -> 52).
 int launch_small(const PackedCall& a, hipStream_t st) {
-  return a.n <= 16 ? launch_small_tt<X, 1>(a, st) : launch_small_tt<X, 2>(a, st);
+  const bool many = a.p.row_tiles >= 4 * device_cu_count();
+  if (a.x_type == CAFEQ_I8) {
+    if (a.n <= 16) return many && a.n > 4 ? launch_small_tt<XI8, 1, 2>(a, st) : launch_small_tt<XI8, 1, 1>(a, st);
+    return many ? launch_small_tt<XI8, 2, 2>(a, st) : launch_small_tt<XI8, 2, 1>(a, st);
+  }
+  if (a.x_type == CAFEQ_BF16) return a.n <= 16 ? launch_small_tt<XBf16, 1, 1>(a, st) : launch_small_tt<XBf16, 2, 1>(a, st);
+  return launch_small_tt<XF32, 1, 1>(a, st);
 }
 
-// Whether the products run in tiles of many tokens.
-bool by_tiles(int64_t n) { return n > 64; }
+// Whether the products run in tiles of 32 and more tokens.  Few tokens do not: every wave has its own run of columns there, without a stage's
+// barriers.  us this way / in tiles: 8 bits, 2048 x 4608 and 128 tokens 10 / 13.5, 3584 x 14336 and 32 16 / 16, 64 25 / 20; bfloat16, 2048 x 4608
+// and 64 tokens 11 / 14, 128 19 / 15, 36864 x 4608 and 8 31 / 33, 16 43 / 33; float32, 2048 x 4608 and 64 21 / 24, 3584 x 14336 and 32 55 / 37.
+bool by_tiles(int x_type, int64_t n, const PackedShape& p) {
+  const double work = double(n) * double(p.rows) * double(p.cols);
+  return x_type == CAFEQ_I8 ? n > 16 && work > 1.6e9 : n > 8 && work > 0.9e9;
+}
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -168,7 +235,7 @@ int cafeq_pack_nibbles(const int8_t* codes, const float* scales, int64_t out, in
 size_t cafeq_infer_packed_workspace_bytes(int x_type, int64_t n, int64_t out, int64_t in, int64_t group) {
   PackedShape p;
   if (n < 1 || x_type < CAFEQ_F32 || x_type > CAFEQ_I8 || packed_shape(out, in, group, &p) != CAFEQ_OK) return 0;
-  return by_tiles(n) ? packed_gemm_bytes(x_type, n, p) : 0;
+  return by_tiles(x_type, n, p) ? packed_gemm_bytes(x_type, n, p) : 0;
 }
 
 int cafeq_infer_packed(const void* X, int x_type, int64_t n, int64_t ldx, const float* xscales, int64_t xgroup, const void* packed,
@@ -192,18 +259,15 @@ int cafeq_infer_packed(const void* X, int x_type, int64_t n, int64_t ldx, const 
   hipStream_t st = static_cast<hipStream_t>(stream);
   auto step = [in](int64_t g) { return g == in || g % 128 == 0 ? 128 : g % 64 == 0 ? 64 : 32; };
   const int fg = std::min(step(p.group), step(gx));
-  const PackedCall c{static_cast<const uint8_t*>(packed), p, X, x_type, n, ldx, xscales, in / gx, fg, int((p.group + fg - 1) / fg),
-                     int((gx + fg - 1) / fg), Y, ldy, y_dtype};
-  if (by_tiles(n)) {
+  const int wunits = int((p.group + fg - 1) / fg), xunits = int((gx + fg - 1) / fg);
+  const PackedCall c{static_cast<const uint8_t*>(packed), p, X, x_type, n, ldx, xscales, in / gx, fg, wunits, xunits, unit_inverse(wunits),
+                     unit_inverse(xunits), Y, ldy, y_dtype};
+  if (by_tiles(x_type, n, p)) {
     if (!ws && packed_gemm_bytes(x_type, n, p)) return CAFEQ_ERR_WORKSPACE;
     if (!aligned16(ws)) return CAFEQ_ERR_BAD_ALIGN;
     return launch_packed_gemm(c, ws, st);
   }
-  switch (x_type) {
-    case CAFEQ_I8: return launch_small<XI8>(c, st);
-    case CAFEQ_BF16: return launch_small<XBf16>(c, st);
-    default: return launch_small<XF32>(c, st);
-  }
+  return launch_small(c, st);
 }
 
 }  // extern "C"
