@@ -511,8 +511,8 @@ def infer_single(X, Tinv, codes, scales, group, out=None):
 
 _FLOATS = {torch.float32: F32, torch.bfloat16: BF16}
 
-# The calls below are made once a projection and token: their checks read each property of a tensor once (a property takes 0.05 to 0.15 us, an
-# allocation 2 us, the launch 3.7).  A norm of one row with its sum: 17.2 -> 13.1 us of the host; a product with one token 11.8 -> 8.2.
+# The calls below are made once a projection and token: their checks read each property of a tensor once (a property takes 0.05 to 0.15 us;
+# an allocation 1.2 by empty_like or empty_strided, 2 by empty; the launch 3.7).  A norm of one row with its sum: 17.2 -> 13.1 us of the host; a product with one token 11.8 -> 8.2.
 
 
 def _rows(t, dev, what):
@@ -559,7 +559,7 @@ def norm_quantize(X, gain=None, residual=None, eps=1e-6, gain_offset=0.0, norm=T
             raise CafeqError("residual must have the shape and type of X")
         res, ldr = residual.data_ptr(), _rows(residual, dev, "residual")
         if sum_out is None:
-            sum_out = X.new_empty(shape)
+            sum_out = torch.empty_like(X)
             total, lds = sum_out.data_ptr(), d
     if sum_out is not None and total is None:
         if sum_out.shape != shape or sum_out.dtype is not dtype:
@@ -571,15 +571,16 @@ def norm_quantize(X, gain=None, residual=None, eps=1e-6, gain_offset=0.0, norm=T
         g = group
         if group < 0 or (group and d % group):
             raise CafeqError("group must divide the columns")
-        codes = X.new_empty(shape, dtype=torch.int8)
-        scales = X.new_empty((n, d // group if group else 1), dtype=torch.float32)
+        ng = d // group if group else 1
+        codes = torch.empty_like(X, dtype=torch.int8)
+        scales = torch.empty_strided((n, ng), (ng, 1), dtype=torch.float32, device=X.device)
         pcodes, pscales = codes.data_ptr(), scales.data_ptr()
     vkind = F32
     if values is not None:
         vkind = _FLOATS.get(values)
         if vkind is None:
             raise CafeqError("values must be torch.float32 or torch.bfloat16")
-        out = X.new_empty(shape, dtype=values)
+        out = torch.empty_like(X, dtype=values)
         pout = out.data_ptr()
     elif group is None:
         raise CafeqError("neither codes nor values are asked for")
@@ -651,7 +652,7 @@ def infer_packed(X, weight, xscales=None, xgroup=0, dtype=torch.float32, out=Non
     if ykind is None:
         raise CafeqError("Y must be float32 or bfloat16")
     if out is None:
-        out = X.new_empty((n, rows), dtype=dtype)
+        out = torch.empty_strided((n, rows), (rows, 1), dtype=dtype, device=X.device)
     if n:
         nbytes = lib.cafeq_infer_packed_workspace_bytes(kind, n, rows, d, group)
         ws = X.new_empty(nbytes, dtype=torch.uint8) if nbytes else None   # of this call alone: streams share nothing

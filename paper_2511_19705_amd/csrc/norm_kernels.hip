@@ -2,9 +2,9 @@
 // inverse transform (paper Sec. 4.1, the first factor of Y^ = X M^-1 Q(MW)) and a scale per group of columns.
 //   h = x + r,  y = h (mean_c h_c^2 + eps)^-1/2 (offset + gain),  z_b = Tinv_b y_b,
 //   a_G = max_{c in G} |z_c|,  q = rint(z fl(127 / a)),  s = a / 127.
-// Without a transform one workgroup holds a row in registers and reads it once (norm_row_kernel).  With one, that kernel
-// leaves 1 / rms of every row and act_tile_kernel forms z from x and r again: a block of z needs the whole row only
-// through that one number.
+// Without a transform one workgroup holds a row in registers and reads it once (norm_row_kernel).  With one, act_tile_kernel
+// forms z: a block of z needs the whole row only through 1 / rms, which for many rows a launch of the row kernel leaves and for few
+// every workgroup forms itself.
 #include "cafeq_common.hpp"
 #include "cafeq_internal.hpp"
 
@@ -57,11 +57,6 @@ __device__ __forceinline__ float act_code(float z, float inv) {
   return inv > 0.f ? fminf(fmaxf(q, -127.f), 127.f) : 0.f;
 }
 
-__device__ __forceinline__ uint16_t bf16_rne(float f) {
-  const uint32_t u = __float_as_uint(f);
-  return mag_bits(f) > 0x7F800000u ? uint16_t((u >> 16) | 0x40u) : uint16_t((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16);
-}
-
 template <class Tag, bool ALIGNED>
 __device__ __forceinline__ void load_vec(float (&v)[kVec], const void* base, int64_t at, int64_t left) {
   const auto* p = static_cast<const typename Tag::elem*>(base) + at;
@@ -90,11 +85,11 @@ __device__ __forceinline__ void store_vec(const float (&v)[kVec], void* base, in
     if constexpr (ALIGNED) {
       uint32_t w[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = uint32_t(bf16_rne(v[2 * e])) | (uint32_t(bf16_rne(v[2 * e + 1])) << 16);
+      for (int e = 0; e < 4; ++e) w[e] = bf16_bits(v[2 * e], v[2 * e + 1]);
       *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) if (e < left) p[e] = bf16_rne(v[e]);
+      for (int e = 0; e < kVec; ++e) if (e < left) p[e] = bf16_bits(v[e]);
     }
   }
 }
@@ -262,7 +257,7 @@ using bf16x8 = __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16;
 using f32x16 = __attribute__((__vector_size__(16 * sizeof(float)))) float;
 
 struct TileArgs {
-  RowArgs r;             // r.group: 0 no codes, else a power of two that lies in a tile
+  RowArgs r;             // r.group: 0 no codes, else a power of two that lies in a tile; r.rstd null: the rows' norms formed here
   const float* Tinv;
   int64_t n;
 };
@@ -283,94 +278,256 @@ __device__ __forceinline__ void split3(const float (&x)[8], Frag& hi, Frag& mid,
       m[e] = __float_as_uint(r1) & 0xFFFF0000u;
       l[e] = __float_as_uint(r1 - __uint_as_float(m[e]));
     }
-    hi.u[p] = (h[0] >> 16) | h[1];
-    mid.u[p] = (m[0] >> 16) | m[1];
-    lo.u[p] = (l[0] >> 16) | (l[1] & 0xFFFF0000u);
+    hi.u[p] = __builtin_amdgcn_perm(h[1], h[0], 0x07060302u);
+    mid.u[p] = __builtin_amdgcn_perm(m[1], m[0], 0x07060302u);
+    lo.u[p] = __builtin_amdgcn_perm(l[1], l[0], 0x07060302u);
   }
 }
 
-constexpr int kTok = 32;   // tokens a step
-
-// A workgroup owns TC columns (whole blocks) and walks over tiles of 32 tokens.  z^T = Tinv y^T on the 16-bit matrix pipe with
-// both operands in three bfloat16 parts and the six part products of weight >= 2^-24 (float32 accuracy: a code moves only where
-// float32 arithmetic in another order moves it).  A wave holds its 32 rows of Tinv in registers for all its tiles; y passes
-// through LDS, split once a workgroup.  In the accumulator a lane has 16 columns of ONE token, so that a group's maximum is a
-// scan of registers, one exchange with lane ^ 32 and, for groups over 32, one through LDS.
-// Bound: few tokens the launch and reading Tinv (64 KB a workgroup at blocks of 128), many the bytes of x, r and the outputs.
-template <int K, class Tag>
-__global__ __launch_bounds__(K == 256 ? 512 : 256) void act_tile_kernel(const TileArgs t) {
-  constexpr int TC = K == 256 ? 256 : 128;
-  constexpr int NW = TC / 32, NT = NW * 64;
-  constexpr int STRIDE = TC + 8;                       // 16-bit elements: rows of 32 lanes fall on distinct banks in eights
-  constexpr int KS = K / 16;
-  constexpr int PER = kTok * TC / NT;                  // columns a thread stages: 16
-  __shared__ uint16_t ys[3][kTok * STRIDE];
-  __shared__ float zs[kTok * (TC + 4)];
-  __shared__ uint32_t top[NW][kTok];
-  const RowArgs& a = t.r;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, l32 = lane & 31;
-  const int64_t col0 = int64_t(blockIdx.x) * TC;       // the tile's first column
-  const int64_t wcol = col0 + wave * 32;               // this wave's output columns
-  const bool live = wcol < a.d;
-  const int blk0 = wave * 32 / K * K;                  // first column of the wave's block inside the tile
-  Frag ph[KS], pm[KS], pl[KS];
+// N consecutive elements (4 or 8) as loaded, and their stores
+template <class Tag, int N> struct Raw;
+template <int N> struct Raw<F32Tag, N> {
+  float4 a[N / 4];
+  __device__ __forceinline__ void load(const void* base, int64_t at) {
 #pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    float w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (live) {
-      const float* p = t.Tinv + (wcol + l32) * K + s * 16 + half * 8;   // row (wcol + l32) of the list of d rows of K floats
-      const float4 u = *reinterpret_cast<const float4*>(p), v = *reinterpret_cast<const float4*>(p + 4);
-      w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w; w[4] = v.x; w[5] = v.y; w[6] = v.z; w[7] = v.w;
-    }
-    split3(w, ph[s], pm[s], pl[s]);
+    for (int i = 0; i < N / 4; ++i) a[i] = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at)[i];
   }
-  const int srow = tid * PER / TC, scol = tid * PER % TC;
-  const int64_t ntile = (t.n + kTok - 1) / kTok;
-  for (int64_t tile = blockIdx.y; tile < ntile; tile += gridDim.y) {
-    const int64_t t0 = tile * kTok;
-    // y of 32 tokens, split, into LDS
-    {
-      const int64_t row = t0 + srow, col = col0 + scol;
-      const bool in = row < t.n && col < a.d;
-      const float rstd = a.norm && in ? a.rstd[row] : 1.f;
+  __device__ __forceinline__ void get(float* v) const {
 #pragma unroll
-      for (int c = 0; c < PER; c += 8) {
-        float v[8];
-        if (in) {
-          load_vec<Tag, true>(v, a.x, row * a.ldx + col + c, 8);
-          if (a.res) {
-            float r[8];
-            load_vec<Tag, true>(r, a.res, row * a.ldr + col + c, 8);
+    for (int i = 0; i < N / 4; ++i) { v[4 * i] = a[i].x; v[4 * i + 1] = a[i].y; v[4 * i + 2] = a[i].z; v[4 * i + 3] = a[i].w; }
+  }
+};
+template <int N> struct Raw<BF16Tag, N> {
+  uint32_t a[N / 2];
+  __device__ __forceinline__ void load(const void* base, int64_t at) {
+    const uint16_t* p = static_cast<const uint16_t*>(base) + at;
+    if constexpr (N == 8) {
+      const uint4 u = *reinterpret_cast<const uint4*>(p);
+      a[0] = u.x; a[1] = u.y; a[2] = u.z; a[3] = u.w;
+    } else {
+      const uint2 u = *reinterpret_cast<const uint2*>(p);
+      a[0] = u.x; a[1] = u.y;
+    }
+  }
+  __device__ __forceinline__ void get(float* v) const {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += r[e];
+    for (int i = 0; i < N / 2; ++i) {
+      v[2 * i] = __uint_as_float(a[i] << 16);
+      v[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
+    }
+  }
+};
+template <int N>
+__device__ __forceinline__ void store_cols(const float* v, void* base, int dtype, int64_t at) {
+  if (dtype == CAFEQ_F32) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4)
+      *reinterpret_cast<float4*>(static_cast<float*>(base) + at + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+  } else {
+    uint32_t w[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) w[i] = bf16_bits(v[2 * i], v[2 * i + 1]);
+    uint16_t* p = static_cast<uint16_t*>(base) + at;
+    if constexpr (N == 8) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+  }
+}
+
+// three parts (split3) of N values at columns `at` of the planes
+template <int N, int PLANE>
+__device__ __forceinline__ void put_parts(const float* v, uint16_t* ys, int at) {
+#pragma unroll
+  for (int part = 0; part < 3; ++part) {
+    // (the compiler keeps what the parts share)
+    uint32_t w[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      uint32_t p[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float r = v[2 * i + e];
+        for (int k = 0; k < part; ++k) r -= __uint_as_float(__float_as_uint(r) & 0xFFFF0000u);
+        p[e] = __float_as_uint(r);
+      }
+      w[i] = __builtin_amdgcn_perm(p[1], p[0], 0x07060302u);
+    }
+    if constexpr (N == 8) *reinterpret_cast<uint4*>(ys + part * PLANE + at) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<uint2*>(ys + part * PLANE + at) = make_uint2(w[0], w[1]);
+  }
+}
+
+constexpr int kTok = 32;        // tokens a step
+constexpr int kFuseTok = 8;     // tokens whose norms every workgroup forms for itself
+constexpr int kOut = 128;       // output columns of a workgroup
+
+// Waves that share a block's contraction: few tokens (one tile) all that the longest chain of loads and products can be cut into, many
+// as far as the rows of Tinv that a wave holds (12 registers for 16 of its columns) leave room for two (256) and four waves a SIMD.
+constexpr int tile_split(int k, bool few) { return few ? (k >= 128 ? 4 : k == 64 ? 2 : 1) : (k >= 128 ? 2 : 1); }
+constexpr int tile_waves(int k, bool few) { return few || k == 256 ? 2 : 4; }
+
+// A workgroup owns 128 output columns and walks over tiles of 32 tokens.  z^T = Tinv y^T on the 16-bit matrix pipe with both
+// operands in three bfloat16 parts and the six part products of weight >= 2^-24 (float32 accuracy: a code moves only where
+// float32 arithmetic in another order moves it).  A wave holds 32 rows of Tinv and its share of their columns in registers for all
+// its tiles; y passes through LDS, split once a workgroup, the next tile's x and r requested before this one's products; the waves'
+// shares of z meet in LDS, in order.  In the accumulator a lane has 16 columns of ONE token.  Up to 8 tokens the workgroup forms the rows'
+// norms itself: reading them costs it less than a launch.
+// Bound: few tokens the launch and reading Tinv (64 KB a workgroup at blocks of 128), many the vector instructions around the products.
+template <int K, int KW, class Tag, bool FUSED, int WAVES>
+__global__ __launch_bounds__(256 * KW, WAVES) void act_tile_kernel(const TileArgs t) {
+  constexpr int YC = K > kOut ? K : kOut;              // columns of y that the outputs need
+  constexpr int NW = 4 * KW, NT = 64 * NW;
+  constexpr int STRIDE = YC + 8;                       // 16-bit elements: rows of 32 lanes fall on distinct banks in eights
+  constexpr int ZS = kOut + 4;
+  constexpr int KS = K / 16 / KW;
+  constexpr int PER = kTok * YC / NT, V = PER < 8 ? PER : 8, NC = PER / V;         // columns a thread stages,
+  constexpr int OPER = kTok * kOut / NT, OV = OPER < 8 ? OPER : 8, ONC = OPER / OV;  // and puts out
+  constexpr int PLANE = kTok * STRIDE;
+  constexpr int ROOM = 3 * PLANE * 2 > KW * kTok * ZS * 4 ? 3 * PLANE * 2 : KW * kTok * ZS * 4;   // z takes the room of y
+  static_assert(V >= 4 && OV >= 4, "sizes");
+  __shared__ __align__(16) unsigned char room[ROOM];
+  __shared__ __align__(16) float gs[YC];
+  __shared__ float norms[kFuseTok][NW];                // sums of squares, by the waves of a row
+  uint16_t* ys = reinterpret_cast<uint16_t*>(room);
+  float* zs = reinterpret_cast<float*>(room);
+  const RowArgs& a = t.r;
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), cw = wave & 3, kw = wave >> 2;
+  const int64_t col0 = int64_t(blockIdx.x) * kOut;     // first output column
+  const int64_t ycol0 = col0 / YC * YC;                // first column of y
+  const int64_t wcol = col0 + cw * 32;                 // this wave's output columns
+  const bool live = wcol < a.d;
+  const int in0 = (K > kOut ? 0 : cw * 32 / K * K) + kw * (K / KW);   // the wave's columns of y, inside the tile
+  const int srow = tid * PER / YC, scol = tid * PER % YC;
+  const int orow = tid * OPER / kOut, ocol = tid * OPER % kOut;
+  const int64_t ycol = ycol0 + scol, ntile = (t.n + kTok - 1) / kTok;
+  const bool mine = K <= kOut || (scol / kOut == int(blockIdx.x & 1));   // whose sums this workgroup writes
+
+  Raw<Tag, V> rx[NC], rr[NC];
+  float rstd = 1.f;
+  // the places of this thread's columns, a tile's worth on after each
+  const int64_t step = int64_t(gridDim.y) * kTok;
+  int64_t row = int64_t(blockIdx.y) * kTok + srow, xat = row * a.ldx + ycol, rat = row * a.ldr + ycol, sat = row * a.lds + ycol;
+  int64_t out = int64_t(blockIdx.y) * kTok + orow, cat = out * a.d + col0 + ocol, vat = out * a.ldv + col0 + ocol;
+  const int gshift = a.codes ? __builtin_ctz(int(a.group)) : 0;            // a power of two
+  const int64_t ngroup = a.d >> gshift;
+  int64_t gat = out * ngroup + ((col0 + ocol) >> gshift);
+  auto request = [&](int64_t at, int64_t x_at, int64_t r_at) __attribute__((always_inline)) {
+    if (at < t.n && ycol < a.d) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        rx[c].load(a.x, x_at + V * c);
+        if (a.res) rr[c].load(a.res, r_at + V * c);
+      }
+      if (!FUSED && a.norm) rstd = a.rstd[at];
+    }
+  };
+  request(row, xat, rat);
+  for (int c = tid; c < YC; c += NT) gs[c] = a.norm && a.gain && ycol0 + c < a.d ? a.offset + a.gain[ycol0 + c] : 1.f;
+  Frag ph[KS], pm[KS], pl[KS];
+  int per = 1;                                         // (fused) waves of a row
+  {
+    float4 w[KS][2];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const float* p = t.Tinv + (wcol + l32) * K + kw * (K / KW) + s * 16 + half * 8;   // row (wcol + l32) of the list of d rows of K floats
+      w[s][0] = live ? *reinterpret_cast<const float4*>(p) : make_float4(0.f, 0.f, 0.f, 0.f);
+      w[s][1] = live ? *reinterpret_cast<const float4*>(p + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    if constexpr (FUSED) {
+      // (blockIdx.y has one value then: all tokens are in the first tile.)  Waves that have no row of their own share one
+      const int n = int(t.n);
+      while (per * 2 * n <= NW) per *= 2;
+      constexpr int ROWS = kFuseTok / NW > 0 ? kFuseTok / NW : 1, FLY = Tag::dtype == CAFEQ_F32 ? 2 : 4;   // rows of a wave; requests of each under way
+      const int first = wave % per * 512 + lane * 8;
+      float sum[ROWS] = {};
+      for (int64_t at0 = first; at0 < a.d; at0 += per * 512 * FLY) {
+        Raw<Tag, 8> u[ROWS][FLY], q[ROWS][FLY];
+#pragma unroll
+        for (int i = 0; i < FLY; ++i)
+#pragma unroll
+          for (int r = 0; r < ROWS; ++r) {
+            const int64_t at = at0 + i * per * 512;
+            const int row = wave / per + r * (NW / per);
+            if (row < n && at < a.d) {
+              u[r][i].load(a.x, row * a.ldx + at);
+              if (a.res) q[r][i].load(a.res, row * a.ldr + at);
+            }
           }
-          if (a.norm) {
-            float g[8];
-            if (a.gain) load_vec<F32Tag, true>(g, a.gain, col + c, 8);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = a.gain ? v[e] * rstd * (a.offset + g[e]) : v[e] * rstd;
+        for (int i = 0; i < FLY; ++i)
+#pragma unroll
+          for (int r = 0; r < ROWS; ++r)
+            if (wave / per + r * (NW / per) < n && at0 + i * per * 512 < a.d) {
+              float v[8], z[8];
+              u[r][i].get(v);
+              if (a.res) q[r][i].get(z);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                if (a.res) v[e] += z[e];
+                sum[r] = fmaf(v[e], v[e], sum[r]);
+              }
+            }
+      }
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        const int row = wave / per + r * (NW / per);
+        const float s = wave_sum(sum[r]);
+        if (lane == 0 && row < n) norms[row][wave % per] = s;
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const float v[8] = {w[s][0].x, w[s][0].y, w[s][0].z, w[s][0].w, w[s][1].x, w[s][1].y, w[s][1].z, w[s][1].w};
+      split3(v, ph[s], pm[s], pl[s]);
+    }
+  }
+  __syncthreads();
+  for (int64_t tile = blockIdx.y; tile < ntile; tile += gridDim.y) {
+    {
+      const bool in = row < t.n && ycol < a.d;
+      if (FUSED && in) {
+        float s = norms[srow][0];
+        for (int w = 1; w < per; ++w) s += norms[srow][w];
+        rstd = 1.f / sqrtf(s / float(a.d) + a.eps);
+      }
+      // y of 32 tokens, split, into LDS
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        float v[V];
+        if (in) {
+          rx[c].get(v);
+          if (a.res) {
+            float r[V];
+            rr[c].get(r);
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] += r[e];
+          }
+          if (a.sum && mine) store_cols<V>(v, a.sum, Tag::dtype, sat + V * c);
+          if (a.norm) {
+#pragma unroll
+            for (int e = 0; e < V; e += 4) {
+              const float4 g = *reinterpret_cast<const float4*>(&gs[scol + V * c + e]);
+              v[e] = v[e] * rstd * g.x; v[e + 1] = v[e + 1] * rstd * g.y; v[e + 2] = v[e + 2] * rstd * g.z; v[e + 3] = v[e + 3] * rstd * g.w;
+            }
           }
         } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = 0.f;
+          for (int e = 0; e < V; ++e) v[e] = 0.f;
         }
-        Frag h, m, l;
-        split3(v, h, m, l);
-        const int at = srow * STRIDE + scol + c;
-        *reinterpret_cast<uint4*>(&ys[0][at]) = make_uint4(h.u[0], h.u[1], h.u[2], h.u[3]);
-        *reinterpret_cast<uint4*>(&ys[1][at]) = make_uint4(m.u[0], m.u[1], m.u[2], m.u[3]);
-        *reinterpret_cast<uint4*>(&ys[2][at]) = make_uint4(l.u[0], l.u[1], l.u[2], l.u[3]);
+        put_parts<V, PLANE>(v, ys, srow * STRIDE + scol + V * c);
       }
     }
     __syncthreads();
+    row += step; xat += step * a.ldx; rat += step * a.ldr; sat += step * a.lds;
+    if (tile + gridDim.y < ntile) request(row, xat, rat);
     f32x16 acc = {};
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       Frag yh, ym, yl;
-      const int at = l32 * STRIDE + blk0 + s * 16 + half * 8;
-      yh.v = *reinterpret_cast<const bf16x8*>(&ys[0][at]);
-      ym.v = *reinterpret_cast<const bf16x8*>(&ys[1][at]);
-      yl.v = *reinterpret_cast<const bf16x8*>(&ys[2][at]);
+      const int at = l32 * STRIDE + in0 + s * 16 + half * 8;
+      yh.v = *reinterpret_cast<const bf16x8*>(ys + at);
+      ym.v = *reinterpret_cast<const bf16x8*>(ys + PLANE + at);
+      yl.v = *reinterpret_cast<const bf16x8*>(ys + 2 * PLANE + at);
       acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(pm[s].v, ym.v, acc, 0, 0, 0);
       acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(pl[s].v, yh.v, acc, 0, 0, 0);
       acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ph[s].v, yl.v, acc, 0, 0, 0);
@@ -378,76 +535,90 @@ __global__ __launch_bounds__(K == 256 ? 512 : 256) void act_tile_kernel(const Ti
       acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ph[s].v, ym.v, acc, 0, 0, 0);
       acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ph[s].v, yh.v, acc, 0, 0, 0);
     }
+    __syncthreads();                                   // y has been read: z takes its room
     // register f of the lane: column 8 (f / 4) + 4 half + f % 4 of the wave's 32, token l32
-    if (a.codes) {
-      uint32_t m = 0u;
-#pragma unroll
-      for (int f = 0; f < 16; ++f) m = max(m, mag_bits(acc[f]));
-      m = max(m, uint32_t(__shfl_xor(int(m), 32)));
-      if (half == 0) top[wave][l32] = m;
-    }
 #pragma unroll
     for (int f = 0; f < 16; f += 4)
-      *reinterpret_cast<float4*>(&zs[l32 * (TC + 4) + wave * 32 + 2 * f + 4 * half]) = make_float4(acc[f], acc[f + 1], acc[f + 2], acc[f + 3]);
+      *reinterpret_cast<float4*>(&zs[(kw * kTok + l32) * ZS + cw * 32 + 2 * f + 4 * half]) = make_float4(acc[f], acc[f + 1], acc[f + 2], acc[f + 3]);
     __syncthreads();
-    // out, sixteen columns a thread
-    const int64_t row = t0 + srow, col = col0 + scol;
-    if (row < t.n && col < a.d) {
-      float inv = 0.f, s = 0.f;
-      if (a.codes) {
-        uint32_t m = 0u;
-        const int w0 = int(scol / a.group * a.group) / 32, w1 = w0 + int(a.group) / 32;
-        for (int w = w0; w < w1; ++w) m = max(m, top[w][srow]);
-        const float amax = __uint_as_float(m);
-        inv = act_inv(amax);
-        s = __fdiv_rn(amax, 127.f);
-        if (scol % a.group == 0) a.scales[row * (a.d / a.group) + col / a.group] = s;
+    // out; a thread's columns lie in one run of 32, and so in one group
+    const bool in = out < t.n && col0 + ocol < a.d;
+    float v[OPER];
+#pragma unroll
+    for (int e = 0; e < OPER; e += 4) {
+      float4 u = *reinterpret_cast<const float4*>(&zs[orow * ZS + ocol + e]);
+#pragma unroll
+      for (int k = 1; k < KW; ++k) {
+        const float4 w = *reinterpret_cast<const float4*>(&zs[(k * kTok + orow) * ZS + ocol + e]);
+        u.x += w.x; u.y += w.y; u.z += w.z; u.w += w.w;
       }
-#pragma unroll
-      for (int c = 0; c < PER; c += 8) {
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; e += 4) {
-          const float4 u = *reinterpret_cast<const float4*>(&zs[srow * (TC + 4) + scol + c + e]);
-          v[e] = u.x; v[e + 1] = u.y; v[e + 2] = u.z; v[e + 3] = u.w;
-        }
-        if (a.codes) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = act_code(v[e], inv);
-          *reinterpret_cast<uint2*>(a.codes + row * a.d + col + c) = make_uint2(pack4(v[0], v[1], v[2], v[3]), pack4(v[4], v[5], v[6], v[7]));
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = __fmul_rn(v[e], s);
-        }
-        if (a.values) store_vec<true>(v, a.values, a.vdtype, row * a.ldv + col + c, 8);
-      }
+      v[e] = u.x; v[e + 1] = u.y; v[e + 2] = u.z; v[e + 3] = u.w;
     }
+    if (a.codes) {
+      // a group is g / OPER neighbouring threads (OPER divides 32): at most 32 lanes of a wave
+      const int g = 1 << gshift;
+      uint32_t m = 0u;
+#pragma unroll
+      for (int e = 0; e < OPER; ++e) m = max(m, mag_bits(v[e]));
+      m = cluster_umax(m, g / OPER);
+      const float amax = __uint_as_float(m), inv = act_inv(amax), s = __fdiv_rn(amax, 127.f);
+      if (in && (ocol & (g - 1)) == 0) a.scales[gat] = s;
+      uint32_t q[OPER / 4];
+#pragma unroll
+      for (int e = 0; e < OPER; ++e) v[e] = act_code(v[e], inv);
+#pragma unroll
+      for (int e = 0; e < OPER / 4; ++e) q[e] = pack4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+      if (in) {
+        int8_t* p = a.codes + cat;
+        if constexpr (OPER == 16) *reinterpret_cast<uint4*>(p) = make_uint4(q[0], q[1], q[2], q[3]);
+        else if constexpr (OPER == 8) *reinterpret_cast<uint2*>(p) = make_uint2(q[0], q[1]);
+        else *reinterpret_cast<uint32_t*>(p) = q[0];
+      }
+#pragma unroll
+      for (int e = 0; e < OPER; ++e) v[e] = __fmul_rn(v[e], s);
+    }
+    if (a.values && in)
+#pragma unroll
+      for (int c = 0; c < ONC; ++c) store_cols<OV>(v + OV * c, a.values, a.vdtype, vat + OV * c);
+    out += step; cat += step * a.d; vat += step * a.ldv; gat += step * ngroup;
     __syncthreads();
   }
 }
 
-template <class Tag>
-int launch_tiles(int k, const TileArgs& t, hipStream_t st) {
-  const int tc = k == 256 ? 256 : 128;
-  const int64_t cols = (t.r.d + tc - 1) / tc, ntile = (t.n + kTok - 1) / kTok;
-  // four workgroups a compute unit: each splits its rows of Tinv once for the token tiles that it takes
-  const int64_t want = (4 * device_cu_count() + cols - 1) / cols;
-  const dim3 grid(unsigned(cols), unsigned(std::min<int64_t>(ntile, std::max<int64_t>(1, want))));
-  switch (k) {
-    case 32: hipLaunchKernelGGL((act_tile_kernel<32, Tag>), grid, dim3(256), 0, st, t); break;
-    case 64: hipLaunchKernelGGL((act_tile_kernel<64, Tag>), grid, dim3(256), 0, st, t); break;
-    case 128: hipLaunchKernelGGL((act_tile_kernel<128, Tag>), grid, dim3(256), 0, st, t); break;
-    case 256: hipLaunchKernelGGL((act_tile_kernel<256, Tag>), grid, dim3(512), 0, st, t); break;
-    default: return CAFEQ_ERR_UNSUPPORTED;
+template <class Tag, int K>
+int launch_tile_k(const TileArgs& t, hipStream_t st) {
+  const int64_t cols = (t.r.d + kOut - 1) / kOut, ntile = (t.n + kTok - 1) / kTok;
+  constexpr int KF = tile_split(K, true), KM = tile_split(K, false);
+  if (ntile == 1) {
+    const dim3 grid{unsigned(cols)}, block(256 * KF);
+    if (t.r.norm && !t.r.rstd) hipLaunchKernelGGL((act_tile_kernel<K, KF, Tag, true, tile_waves(K, true)>), grid, block, 0, st, t);
+    else hipLaunchKernelGGL((act_tile_kernel<K, KF, Tag, false, tile_waves(K, true)>), grid, block, 0, st, t);
+  } else {
+    // what fits the chip at once: each workgroup splits its rows of Tinv once for the token tiles that it takes
+    const int64_t want = std::max<int64_t>(1, tile_waves(K, false) / KM * device_cu_count() / cols);
+    const dim3 grid(unsigned(cols), unsigned(std::min<int64_t>(ntile, want)));
+    hipLaunchKernelGGL((act_tile_kernel<K, KM, Tag, false, tile_waves(K, false)>), grid, dim3(256 * KM), 0, st, t);
   }
   CAFEQ_CHECK_LAUNCH();
   return CAFEQ_OK;
 }
 
-// whether act_tile_kernel has all of a group in one tile
-bool group_in_tile(int k, int64_t group) {
-  const int64_t tc = k == 256 ? 256 : 128;
-  return group <= tc && (group & (group - 1)) == 0;
+template <class Tag>
+int launch_tiles(int k, const TileArgs& t, hipStream_t st) {
+  switch (k) {
+    case 32: return launch_tile_k<Tag, 32>(t, st);
+    case 64: return launch_tile_k<Tag, 64>(t, st);
+    case 128: return launch_tile_k<Tag, 128>(t, st);
+    case 256: return launch_tile_k<Tag, 256>(t, st);
+    default: return CAFEQ_ERR_UNSUPPORTED;
+  }
 }
+
+// whether act_tile_kernel has all of a group in one tile
+bool group_in_tile(int64_t group) { return group <= kOut && (group & (group - 1)) == 0; }
+
+// 1 / rms of the rows, where a launch of its own forms them
+size_t norms_bytes(int64_t n) { return n > kFuseTok ? align_up(size_t(n) * sizeof(float), 256) : 0; }
 
 bool overlaps(const void* a, int64_t bytes_a, const void* b, int64_t bytes_b) {
   const auto p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
@@ -463,9 +634,8 @@ extern "C" {
 
 size_t cafeq_norm_workspace_bytes(int64_t n, int64_t d, const cafeq_xform* xf, int64_t group) {
   if (n < 1 || d < 1 || !xf) return 0;
-  const size_t rstd = align_up(size_t(n) * sizeof(float), 256);
-  const bool whole = group >= 0 && !group_in_tile(xf->k, group == 0 ? d : group);
-  return rstd + (whole ? align_up(size_t(n) * size_t(d) * sizeof(float), 256) : 0);
+  const bool whole = group >= 0 && !group_in_tile(group == 0 ? d : group);
+  return norms_bytes(n) + (whole ? align_up(size_t(n) * size_t(d) * sizeof(float), 256) : 0);
 }
 
 int cafeq_norm_quantize(const cafeq_activations* in, int64_t n, int64_t d, const cafeq_xform* xf, int64_t group,
@@ -493,11 +663,11 @@ int cafeq_norm_quantize(const cafeq_activations* in, int64_t n, int64_t d, const
     if (!xf->Tinv) return CAFEQ_ERR_INVALID_ARG;
     if (xf->k != 32 && xf->k != 64 && xf->k != 128 && xf->k != 256) return CAFEQ_ERR_UNSUPPORTED;
     if (xf->rep != 1 || int64_t(xf->nb) * xf->k != d) return CAFEQ_ERR_BAD_SHAPE;
-    if (!aligned(xf->Tinv, 16) || !aligned(codes, 8) || !rows_aligned(in->x, in->ldx, size) ||
-        !rows_aligned(in->residual, in->ldr, size) || !aligned(in->gain, 16) ||
+    if (!aligned(xf->Tinv, 16) || !rows_aligned(in->x, in->ldx, size) ||
+        !rows_aligned(in->residual, in->ldr, size) || !rows_aligned(in->sum, in->lds, size) || !aligned(codes, 16) ||
         !rows_aligned(values, ldv, values_dtype == CAFEQ_F32 ? 4 : 2))
       return CAFEQ_ERR_BAD_ALIGN;
-    if (!ws) return CAFEQ_ERR_WORKSPACE;
+    if (!ws && cafeq_norm_workspace_bytes(n, d, xf, codes ? group : -1)) return CAFEQ_ERR_WORKSPACE;
     if (!aligned(ws, 16)) return CAFEQ_ERR_BAD_ALIGN;
     // x and residual are read a second time, after the sum has been written
     const int64_t span = size * ((n - 1) * in->lds + d);
@@ -515,14 +685,15 @@ int cafeq_norm_quantize(const cafeq_activations* in, int64_t n, int64_t d, const
     a.group = g; a.codes = codes; a.scales = scales; a.values = values; a.ldv = ldv; a.vdtype = values_dtype;
     return launch_rows(a, in->dtype, n, st);
   }
-  a.rstd = static_cast<float*>(ws);
-  if (in->norm || in->sum) {
-    const int rc = launch_rows(a, in->dtype, n, st);
+  if (in->norm && norms_bytes(n)) {
+    a.rstd = static_cast<float*>(ws);
+    RowArgs norms = a;
+    norms.sum = nullptr;                      // written where z is formed
+    const int rc = launch_rows(norms, in->dtype, n, st);
     if (rc) return rc;
   }
-  a.sum = nullptr;
-  float* z = reinterpret_cast<float*>(static_cast<char*>(ws) + align_up(size_t(n) * sizeof(float), 256));
-  const bool direct = !codes || group_in_tile(xf->k, g);
+  float* z = reinterpret_cast<float*>(static_cast<char*>(ws) + norms_bytes(n));
+  const bool direct = !codes || group_in_tile(g);
   TileArgs t{a, xf->Tinv, n};
   t.r.group = codes ? g : 0;
   if (direct) {

@@ -62,19 +62,29 @@ int launch_packed_gemm(const PackedCall& c, void* ws, hipStream_t st);
 __device__ __forceinline__ uint32_t low16(uint32_t w) { return (w << 4) & 0xF0F0F0F0u; }   // 16 q of columns 0 .. 3 of a dword
 __device__ __forceinline__ uint32_t high16(uint32_t w) { return w & 0xF0F0F0F0u; }         // of columns 4 .. 7
 
-// two signed bytes of a dword as bfloat16 (whole numbers up to 128: exact)
+// Codes of columns I and I + 1 of a dword's eight (w: the dword, or the dword >> 4 for the upper four) as a pair of bfloat16, each divided by
+// 16, exactly: the hardware's conversion of a signed nibble gives q / 16.
 template <int I>
 __device__ __forceinline__ uint32_t bf16_pair(uint32_t w) {
-  const float a = float(int(int8_t(w >> (8 * I)))), b = float(int(int8_t(w >> (8 * I + 8))));
-  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+  uint32_t a, b;
+  if constexpr (I == 0) {
+    asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(a) : "v"(w));
+    asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(b) : "v"(w));
+  } else {
+    asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(a) : "v"(w));
+    asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(b) : "v"(w));
+  }
+  return __builtin_amdgcn_perm(b, a, 0x07060302u);
 }
-// eight codes times 16 as a bfloat16 operand
+// eight codes / 16 as a bfloat16 operand
 __device__ __forceinline__ bf16x8_t bf16_codes(uint32_t w) {
-  const uint32_t lo = low16(w), hi = high16(w);
+  const uint32_t hi = w >> 4;
   union { uint32_t u[4]; bf16x8_t v; } f;
-  f.u[0] = bf16_pair<0>(lo); f.u[1] = bf16_pair<2>(lo); f.u[2] = bf16_pair<0>(hi); f.u[3] = bf16_pair<2>(hi);
+  f.u[0] = bf16_pair<0>(w); f.u[1] = bf16_pair<2>(w); f.u[2] = bf16_pair<0>(hi); f.u[3] = bf16_pair<2>(hi);
   return f.v;
 }
+// what a result is multiplied by in the end: 8-bit operands hold 16 q, bfloat16 ones q / 16
+__host__ __device__ inline float code_unit(bool i8) { return i8 ? 0.0625f : 16.f; }
 
 // two float32 values' leading bits as a pair of bfloat16, and what they leave (nothing of an infinity)
 __device__ __forceinline__ uint32_t split_pair(float& a, float& b) {
@@ -87,10 +97,8 @@ __device__ __forceinline__ uint32_t split_pair(float& a, float& b) {
 }
 
 __device__ __forceinline__ void store_y(void* y, int dtype, int64_t at, float v) {
-  if (dtype == CAFEQ_F32) { static_cast<float*>(y)[at] = v; return; }
-  const uint32_t u = __float_as_uint(v);
-  static_cast<uint16_t*>(y)[at] =
-      (u & 0x7FFFFFFFu) > 0x7F800000u ? uint16_t((u >> 16) | 0x40u) : uint16_t((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16);
+  if (dtype == CAFEQ_F32) static_cast<float*>(y)[at] = v;
+  else static_cast<uint16_t*>(y)[at] = bf16_bits(v);
 }
 
 // The forms of the activations.  Chunk: 16 consecutive columns of a token (a lane's share of 64) as loaded; Form: as the matrix

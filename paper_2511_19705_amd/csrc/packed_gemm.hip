@@ -228,13 +228,16 @@ __global__ __launch_bounds__(kThreads, kPerCu) void packed_gemm_kernel(const Gem
     const int sz = l31 & 7;
     slot = slot + 1 == L::kRing ? 0 : slot + 1;
     // Tiles one after another, (token tile, run, row tile).  While a tile's instructions run, the one before it is taken up in
-    // float32: from the second instruction on, when the last one's result is there.
+    // float32: from the second instruction on, when the last one's result is there.  Where a unit spans both parts of a stage and the
+    // registers hold all tiles' accumulators, they are kept from part to part and taken up once.
     constexpr int PER = NT * RUNS, TILES = MT * PER;
+    constexpr bool KEEP = F::kParts > 1 && UPB == 1;
+    constexpr int ACCS = KEEP ? TILES : 2;
+    typename F::Acc acc[ACCS];
 #pragma unroll
     for (int part = 0; part < F::kParts; ++part) {
       unpack(part);
       typename F::Frag x[4];
-      typename F::Acc acc[2];
       auto read_x = [&](int m, int i) __attribute__((always_inline)) {
         x[i] = *reinterpret_cast<const typename F::Frag*>(xt + m * 32 * ROWB + (F::chunk(part, i, h) ^ sz) * 16);
       };
@@ -246,11 +249,12 @@ __global__ __launch_bounds__(kThreads, kPerCu) void packed_gemm_kernel(const Gem
           if constexpr (SX) f = *reinterpret_cast<const f32x4*>(xs + u * kThreads + m * 32 + 8 * v + 4 * h);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float z = float(acc[j & 1][4 * v + e]);
+            const float z = float(acc[j % ACCS][4 * v + e]);
             y[m][t][4 * v + e] = fmaf(SX ? z * f[e] : z, sc[t][u], y[m][t][4 * v + e]);
           }
         }
       };
+      const bool taken = !KEEP || part == F::kParts - 1;
 #pragma unroll
       for (int i = 0; i < 4; ++i) read_x(0, i);
 #pragma unroll
@@ -258,10 +262,10 @@ __global__ __launch_bounds__(kThreads, kPerCu) void packed_gemm_kernel(const Gem
         const int m = j / PER, u = j / NT % RUNS, t = j % NT;
 #pragma unroll
         for (int i = 0; i < SPU; ++i) {
-          acc[j & 1] = F::mul(x[u * SPU + i], b[t][u * SPU + i], i == 0 ? typename F::Acc{} : acc[j & 1]);
+          acc[j % ACCS] = F::mul(x[u * SPU + i], b[t][u * SPU + i], i == 0 && !(KEEP && part) ? typename F::Acc{} : acc[j % ACCS]);
           if (t == NT - 1 && m + 1 < MT) read_x(m + 1, u * SPU + i);
           __builtin_amdgcn_sched_barrier(0);
-          if (j > 0) {
+          if (j > 0 && taken) {
             if (SPU == 4) take(j - 1, i == 0 ? 0 : i - 1, i == 0 ? 0 : i == 3 ? 4 : i);
             else if (SPU == 2) take(j - 1, i, i == 0 ? 1 : 4);
             else take(j - 1, 0, 4);
@@ -269,7 +273,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void packed_gemm_kernel(const Gem
           __builtin_amdgcn_sched_barrier(0);
         }
       }
-      take(TILES - 1, 0, 4);
+      if (taken) take(TILES - 1, 0, 4);
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // requests past the last stage
@@ -289,7 +293,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void packed_gemm_kernel(const Gem
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int tok = m * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
-      const float f = (I8 && !SX && tok <= last ? a.xscales[t0 + tok] : 1.f) * 0.0625f;
+      const float f = (I8 && !SX && tok <= last ? a.xscales[t0 + tok] : 1.f) * code_unit(I8);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const int64_t row = row0 + t * 32 + l31;
@@ -299,7 +303,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void packed_gemm_kernel(const Gem
 }
 
 // the pieces of a tile in order, to Y
-__global__ __launch_bounds__(256) void packed_join_kernel(const GemmArgs a, int mt, int nt, bool per_token) {
+__global__ __launch_bounds__(256) void packed_join_kernel(const GemmArgs a, int mt, int nt, bool per_token, float unit) {
   const int size = 32 * mt * 32 * nt * kWaves;
   const int tile = blockIdx.y, e = blockIdx.x * 256 + threadIdx.x;
   int tt, rt;
@@ -311,7 +315,7 @@ __global__ __launch_bounds__(256) void packed_join_kernel(const GemmArgs a, int 
   const float* p = a.part + int64_t(tile) * a.split * size + e;
   float v = 0.f;
   for (int k = 0; k < a.split; ++k) v += p[int64_t(k) * size];
-  store_y(a.y, a.ydtype, tok * a.ldy + row, v * ((per_token ? a.xscales[tok] : 1.f) * 0.0625f));
+  store_y(a.y, a.ydtype, tok * a.ldy + row, v * ((per_token ? a.xscales[tok] : 1.f) * unit));
 }
 
 // float32 activations as three planes of bfloat16, the small parts first: hi + mid + lo exactly
@@ -439,7 +443,7 @@ int launch_packed_gemm(const PackedCall& c, void* ws, hipStream_t st) {
   if (rc) return rc;
   if (rest) {
     const int size = 32 * g.mt * 32 * g.nt * kWaves;
-    hipLaunchKernelGGL(packed_join_kernel, dim3(size / 256, rest), dim3(256), 0, st, a, g.mt, g.nt, i8 && !sx);
+    hipLaunchKernelGGL(packed_join_kernel, dim3(size / 256, rest), dim3(256), 0, st, a, g.mt, g.nt, i8 && !sx, code_unit(i8));
     CAFEQ_CHECK_LAUNCH();
   }
   return CAFEQ_OK;

@@ -161,7 +161,7 @@ __global__ __launch_bounds__(1024) void packed_small_kernel(const PackedCall a) 
     const int64_t row = int64_t(rt0 + ot) * kRowTile + o;
     float v = 0.f;
     for (int i = 0; i < nwave; ++i) v += red[i * OT * TT * 256 + at];
-    if (t0 + tok < a.n && row < a.p.rows) store_y(a.y, a.ydtype, (t0 + tok) * a.ldy + row, v * 0.0625f);
+    if (t0 + tok < a.n && row < a.p.rows) store_y(a.y, a.ydtype, (t0 + tok) * a.ldy + row, v * code_unit(X::kScaled));
   }
 }
 
@@ -190,7 +190,7 @@ int launch_small_tt(const PackedCall& a, hipStream_t st) {
 int launch_small(const PackedCall& a, hipStream_t st) {
   const bool many = a.p.row_tiles >= 4 * device_cu_count();
   if (a.x_type == CAFEQ_I8) {
-    if (a.n <= 16) return many && a.n > 4 ? launch_small_tt<XI8, 1, 2>(a, st) : launch_small_tt<XI8, 1, 1>(a, st);
+    if (a.n <= 16) return many && a.n > 2 ? launch_small_tt<XI8, 1, 2>(a, st) : launch_small_tt<XI8, 1, 1>(a, st);
     return many ? launch_small_tt<XI8, 2, 2>(a, st) : launch_small_tt<XI8, 2, 1>(a, st);
   }
   if (a.x_type == CAFEQ_BF16) return a.n <= 16 ? launch_small_tt<XBf16, 1, 1>(a, st) : launch_small_tt<XBf16, 2, 1>(a, st);
