@@ -60,6 +60,7 @@ template <> struct Form<true> {
     return i32x4{int(low16(d0)), int(high16(d0)), int(low16(d1)), int(high16(d1))};
   }
   static __device__ __forceinline__ int chunk(int, int i, int h) { return 2 * i + h; }
+  static __device__ __forceinline__ int swizzle(int row) { return row >> 1 & 7; }   // two rows fill the 64 banks
   static __device__ __forceinline__ Acc mul(const Frag& x, const Frag& b, const Acc& c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(x, b, c, 0, 0, 0); }
 };
 template <> struct Form<false> {
@@ -71,6 +72,7 @@ template <> struct Form<false> {
     const uint4& q = i >> 1 ? q1 : q0;
     return bf16_codes(p ? (i & 1 ? q.w : q.z) : (i & 1 ? q.y : q.x));
   }
+  static __device__ __forceinline__ int swizzle(int row) { return row & 15; }
   static __device__ __forceinline__ int chunk(int p, int i, int h) { return 4 * (2 * p + (i >> 1)) + 2 * h + (i & 1); }
   static __device__ __forceinline__ Acc mul(const Frag& x, const Frag& b, const Acc& c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, b, c, 0, 0, 0); }
 };
@@ -137,10 +139,10 @@ __global__ __launch_bounds__(kThreads, kPerCu) void packed_gemm_kernel(const Gem
   const int64_t row0 = int64_t(rt) * TROWS + wave * 32 * NT; // the wave's first row
 
   // Requests of the activations: a thread's piece i is 16 bytes of token row i * RSTEP + tid / CH (past the last one: that one's).
-  // The chunks of a token lie in LDS at their number XOR the token, so that the operand reads of eight tokens fall on distinct banks.
+  // The chunks of a token lie in LDS at their number XOR the token's swizzle, so that the operand reads of 16 tokens fall on distinct banks.
   constexpr int RSTEP = kThreads / CH;
   const uint32_t ldx = uint32_t(a.ldx), rmax = uint32_t(last) * ldx, rfirst = uint32_t(tid / CH) * ldx;
-  const uint32_t ch = uint32_t((tid % CH) ^ (tid / CH & 7)) * 16u;
+  const uint32_t ch = uint32_t((tid % CH) ^ F::swizzle(tid / CH)) * 16u;
   const uint32_t tail = uint32_t(a.p.cols - int64_t(nkb - 1) * kBlockK) * (ROWB / kBlockK);   // bytes of a token in the last block
   const uint8_t* xbase = a.x + t0 * a.ldx;
   auto dma = [&](int plane, int kb, int slot) __attribute__((always_inline)) {
@@ -225,7 +227,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void packed_gemm_kernel(const Gem
         for (int i = 0; i < 4; ++i) b[t][i] = F::unpack(w[t][0], w[t][1], part, i);
     };
     const unsigned char* xt = smem + slot * L::kStage + l31 * ROWB;
-    const int sz = l31 & 7;
+    const int sz = F::swizzle(l31);
     slot = slot + 1 == L::kRing ? 0 : slot + 1;
     // Tiles one after another, (token tile, run, row tile).  While a tile's instructions run, the one before it is taken up in
     // float32: from the second instruction on, when the last one's result is there.  Where a unit spans both parts of a stage and the
