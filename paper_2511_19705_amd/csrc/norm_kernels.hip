@@ -648,7 +648,7 @@ int cafeq_norm_quantize(const cafeq_activations* in, int64_t n, int64_t d, const
   if (!codes && !values) return CAFEQ_ERR_INVALID_ARG;
   if (n < 0 || d < 1 || in->ldx < d || (in->residual && in->ldr < d) || (in->sum && in->lds < d) || (values && ldv < d))
     return CAFEQ_ERR_BAD_SHAPE;
-  if (d > kMaxRow || n > INT32_MAX) return CAFEQ_ERR_UNSUPPORTED;
+  if (d > kMaxRow || n > (int64_t(1) << 21)) return CAFEQ_ERR_UNSUPPORTED;   // a launch's threads stay below 2^32
   int64_t g = 0;
   if (codes) {
     if (group < 0 || (group > 0 && (group % kMinGroup != 0 || d % group != 0))) return CAFEQ_ERR_BAD_SHAPE;

@@ -30,6 +30,7 @@ inline int packed_shape(int64_t out, int64_t in, int64_t group, PackedShape* p) 
   p->groups = in / g;
   p->row_tiles = (out + 2 * kRowTile - 1) / (2 * kRowTile) * 2;   // whole tiles of 32 rows
   p->kblocks = (in + kBlockK - 1) / kBlockK;
+  if (p->row_tiles * p->kblocks > (int64_t(1) << 25)) return CAFEQ_ERR_UNSUPPORTED;            // a launch's threads stay below 2^32
   p->scales_at = p->row_tiles * p->kblocks * 1024;
   p->bytes = p->scales_at + p->row_tiles * p->groups * kRowTile * int64_t(sizeof(float));
   return CAFEQ_OK;

@@ -251,7 +251,7 @@ int cafeq_infer_packed(const void* X, int x_type, int64_t n, int64_t ldx, const 
   const int64_t gx = x_type != CAFEQ_I8 || xgroup == 0 ? in : xgroup;
   if (gx < 32 || gx % 32 != 0 || in % gx != 0) return CAFEQ_ERR_BAD_SHAPE;
   const int size = x_type == CAFEQ_F32 ? 4 : x_type == CAFEQ_BF16 ? 2 : 1;
-  if (n > (int64_t(1) << 20) || ldx > (int64_t(1) << 24)) return CAFEQ_ERR_UNSUPPORTED;   // a tile's offsets stay below 2^32 bytes
+  if (n > (int64_t(1) << 19) || ldx > (int64_t(1) << 24)) return CAFEQ_ERR_UNSUPPORTED;   // a grid's rows below 2^16, a tile's offsets below 2^32 bytes
   if (!aligned16(X) || !aligned16(packed) || ldx * size % 16 != 0 || (reinterpret_cast<uintptr_t>(Y) & (y_dtype == CAFEQ_F32 ? 3u : 1u)) != 0 ||
       (reinterpret_cast<uintptr_t>(xscales) & 3u) != 0)
     return CAFEQ_ERR_BAD_ALIGN;

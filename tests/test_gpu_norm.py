@@ -269,3 +269,22 @@ def test_refusals(env):
                 lambda: cafeq.norm_quantize(torch.zeros((1, 65568), device=dev))):
         with pytest.raises(E):
             bad()
+
+
+@pytest.mark.parametrize("k", [0, 32])
+def test_rows_past_two_gigabytes(env, k):
+    torch, cafeq = env
+    n, d = 40000, 16384                                   # 2.6 GB of float32
+    x = torch.zeros((n, d), device="cuda:0")
+    at = [0, 32767, 32768, n - 1]
+    x[at] = torch.randn((4, d), device="cuda:0")
+    P = torch.eye(32, device="cuda:0").repeat(d // 32, 1, 1) if k else None
+    o = cafeq.norm_quantize(x, Tinv=P, group=128)
+    few = cafeq.norm_quantize(x[at].contiguous(), Tinv=P, group=128)
+    # 1 / rms of few rows is summed in another order: scales to 64 u, and a code at a tie may move by one
+    assert (o.scales[at] - few.scales).abs().max() <= 64 * U * few.scales.max()
+    assert (o.codes[at].int() - few.codes.int()).abs().max() <= 1
+    assert (o.codes[at] != few.codes).float().mean() <= 1e-3
+    rest = torch.ones(n, dtype=torch.bool, device="cuda:0")
+    rest[at] = False
+    assert not o.codes[rest].any() and not o.scales[rest].any()

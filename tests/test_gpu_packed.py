@@ -233,3 +233,25 @@ def test_refusals(env):
                 lambda: cafeq.infer_packed(torch.zeros((2, 66), device=dev)[:, 1:65], packed), lambda: cafeq.infer_packed(X.cpu(), packed)):
         with pytest.raises(E):
             bad()
+
+
+def test_activations_and_results_past_two_gigabytes(env):
+    # 70000 tokens of 32768 bytes, and as many results of 8192 rows in float32: offsets that no 32 bits hold
+    torch, cafeq = env
+    rng = np.random.default_rng(8)
+    for rows, cols in ((33, 32768), (8192, 256)):
+        codes, scales = _weight(rows, cols, 128, 3)
+        packed = cafeq.pack_nibbles(_dev(torch, codes), _dev(torch, scales), 128)
+        n = 70000
+        X = torch.zeros((n, cols), dtype=torch.int8, device="cuda:0")
+        at = [0, 1, 65535, 65536, n - 2, n - 1]
+        X[at] = _dev(torch, rng.integers(-127, 128, (len(at), cols)).astype(np.int8))
+        Y = cafeq.infer_packed(X, packed, xscales=torch.ones((n, 1), device="cuda:0"), xgroup=0)
+        ref = X[at].double().cpu().numpy() @ (codes * _spread(scales, 128, cols)).T
+        bound = 2.0 ** -24 * (cols // 128 + 20) * sum(np.abs(X[at].double().cpu().numpy()[:, c:c + 128] @ (codes * _spread(scales, 128, cols))[:, c:c + 128].T)
+                                                       for c in range(0, cols, 128))
+        assert np.all(np.abs(Y[at].double().cpu().numpy() - ref) <= bound)
+        rest = torch.ones(n, dtype=torch.bool, device="cuda:0")
+        rest[at] = False
+        assert not Y[rest].any()
+        del X, Y
