@@ -341,11 +341,11 @@ struct Plan {
   size_t part_at, bytes;
 };
 
-// What a stage of a tile takes, in us: on a compute unit alone, and with a second workgroup there (groups of 128; 4608 columns, 128 to 1024
-// workgroups).
+// What a stage of a tile takes, in us: on a compute unit alone, and with a second workgroup there (groups of 128, 4608 columns, one or two
+// workgroups a compute unit and, of the larger tiles, thousands).
 struct TileCost { int mt, nt; float alone, paired; };
-constexpr TileCost kTilesI8[] = {{1, 1, 0.54f, 0.71f}, {2, 1, 0.76f, 1.03f}, {2, 2, 1.25f, 2.0f}, {4, 2, 2.15f, 3.4f}};
-constexpr TileCost kTilesBf16[] = {{1, 1, 0.75f, 0.98f}, {2, 1, 0.98f, 1.42f}, {2, 2, 1.56f, 2.85f}};   // 4 x 2 leaves no room for a second workgroup: 5.0
+constexpr TileCost kTilesI8[] = {{1, 1, 0.48f, 0.69f}, {2, 1, 0.64f, 0.92f}, {2, 2, 1.1f, 1.75f}, {4, 2, 1.8f, 2.9f}};
+constexpr TileCost kTilesBf16[] = {{1, 1, 0.62f, 0.88f}, {2, 1, 0.83f, 1.27f}, {2, 2, 1.38f, 2.2f}};   // 4 x 2 leaves no room for a second workgroup: 5.0
 
 // The tile and the split with the least estimated time.  Tiles that fill rounds of workgroups run whole; of the rest every one is split along
 // the columns, as far as that fills the compute units and its partial sums (written, read, a launch more) cost less than it gains.

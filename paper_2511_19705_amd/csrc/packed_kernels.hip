@@ -198,11 +198,11 @@ int launch_small(const PackedCall& a, hipStream_t st) {
 }
 
 // Whether the products run in tiles of 32 and more tokens.  Few tokens do not: every wave has its own run of columns there, without a stage's
-// barriers.  us this way / in tiles: 8 bits, 2048 x 4608 and 128 tokens 10 / 13.5, 3584 x 14336 and 32 16 / 16, 64 25 / 20; bfloat16, 2048 x 4608
-// and 64 tokens 11 / 14, 128 19 / 15, 36864 x 4608 and 8 31 / 33, 16 43 / 33; float32, 2048 x 4608 and 64 21 / 24, 3584 x 14336 and 32 55 / 37.
+// barriers, but the weights are read again for every 16 or 32 tokens.  us this way / in tiles: 8 bits, 2048 x 4608 and 64 tokens 8 / 12, 96 13.5 / 13,
+// 3584 x 14336 and 24 19 / 17, 64 25 / 19; bfloat16, 2048 x 4608 and 64 tokens 11 / 14, 128 19 / 15, 36864 x 4608 and 8 31 / 33, 16 43 / 33; float32,
+// 2048 x 4608 and 64 21 / 24, 3584 x 14336 and 32 55 / 34.
 bool by_tiles(int x_type, int64_t n, const PackedShape& p) {
-  const double work = double(n) * double(p.rows) * double(p.cols);
-  return x_type == CAFEQ_I8 ? n > 16 && work > 1.6e9 : n > 8 && work > 0.9e9;
+  return n > (x_type == CAFEQ_I8 ? 16 : 8) && double(n) * double(p.rows) * double(p.cols) > 0.9e9;
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
