@@ -510,6 +510,7 @@ def infer_single(X, Tinv, codes, scales, group, out=None):
 
 
 _FLOATS = {torch.float32: F32, torch.bfloat16: BF16}
+_ERR_WORKSPACE = -7
 
 # The calls below are made once a projection and token: their checks read each property of a tensor once (a property takes 0.05 to 0.15 us;
 # an allocation 1.2 by empty_like or empty_strided, 2 by empty; the launch 3.7).  A norm of one row with its sum: 17.2 -> 13.1 us of the host; a product with one token 11.8 -> 8.2.
@@ -552,7 +553,7 @@ def norm_quantize(X, gain=None, residual=None, eps=1e-6, gain_offset=0.0, norm=T
     ldx = _rows(X, dev, "X")
     n, d = shape = X.shape
     px = X.data_ptr()
-    res = ldr = total = lds = xf = ws = None
+    res = ldr = total = lds = xf = None
     pgain = None if gain is None else _operand(gain, dev, torch.float32, (d,), "gain")
     if residual is not None:
         if residual.shape != shape or residual.dtype is not dtype:
@@ -586,13 +587,15 @@ def norm_quantize(X, gain=None, residual=None, eps=1e-6, gain_offset=0.0, norm=T
         raise CafeqError("neither codes nor values are asked for")
     if Tinv is not None:
         k = Tinv.shape[-1]
-        xf = Xform(None, _operand(Tinv, dev, torch.float32, (d // k if k else 0, k, k), "Tinv"), k, d // k, 1)
-        nbytes = lib.cafeq_norm_workspace_bytes(n, d, ctypes.byref(xf), g)
-        ws = X.new_empty(nbytes, dtype=torch.uint8) if nbytes else None   # of this call alone: streams share nothing
+        xf = ctypes.byref(Xform(None, _operand(Tinv, dev, torch.float32, (d // k if k else 0, k, k), "Tinv"), k, d // k, 1))
     if n:
         a = Activations(px, res, total, ldx, ldr or 0, lds or 0, kind, 1 if norm else 0, pgain, gain_offset, eps)
-        rc = lib.cafeq_norm_quantize(ctypes.byref(a), n, d, None if xf is None else ctypes.byref(xf), g if g > 0 else 0, pcodes, pscales, pout,
-                                     vkind, d, _ptr(ws), torch._C._cuda_getCurrentRawStream(dev))
+        stream = torch._C._cuda_getCurrentRawStream(dev)
+        rc = lib.cafeq_norm_quantize(ctypes.byref(a), n, d, xf, g if g > 0 else 0, pcodes, pscales, pout, vkind, d, None, stream)
+        if rc == _ERR_WORKSPACE:
+            # few rows need none and are what waits for the host; the buffer is of this call alone, so that streams share nothing
+            ws = X.new_empty(lib.cafeq_norm_workspace_bytes(n, d, xf, g), dtype=torch.uint8)
+            rc = lib.cafeq_norm_quantize(ctypes.byref(a), n, d, xf, g if g > 0 else 0, pcodes, pscales, pout, vkind, d, ws.data_ptr(), stream)
         if rc:
             _check(rc)
     return Normed(codes, scales, out, sum_out)
@@ -654,10 +657,12 @@ def infer_packed(X, weight, xscales=None, xgroup=0, dtype=torch.float32, out=Non
     if out is None:
         out = torch.empty_strided((n, rows), (rows, 1), dtype=dtype, device=X.device)
     if n:
-        nbytes = lib.cafeq_infer_packed_workspace_bytes(kind, n, rows, d, group)
-        ws = X.new_empty(nbytes, dtype=torch.uint8) if nbytes else None   # of this call alone: streams share nothing
-        rc = lib.cafeq_infer_packed(X.data_ptr(), kind, n, ldx, ps, xgroup, data.data_ptr(), rows, d, group, out.data_ptr(), ykind, ldy, _ptr(ws),
-                                    torch._C._cuda_getCurrentRawStream(dev))
+        px, pw, py, stream = X.data_ptr(), data.data_ptr(), out.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)
+        rc = lib.cafeq_infer_packed(px, kind, n, ldx, ps, xgroup, pw, rows, d, group, py, ykind, ldy, None, stream)
+        if rc == _ERR_WORKSPACE:
+            # few tokens need none and are what waits for the host; the buffer is of this call alone, so that streams share nothing
+            ws = X.new_empty(lib.cafeq_infer_packed_workspace_bytes(kind, n, rows, d, group), dtype=torch.uint8)
+            rc = lib.cafeq_infer_packed(px, kind, n, ldx, ps, xgroup, pw, rows, d, group, py, ykind, ldy, ws.data_ptr(), stream)
         if rc:
             _check(rc)
     return out

@@ -209,7 +209,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void packed_gemm_kernel(const Gem
     if (++kb == nkb) { kb = 0; ++plane; }
     const unsigned char* wt = smem + slot * L::kStage + L::kX;
     const float* xs = reinterpret_cast<const float*>(wt + L::kW + L::kSw);
-    typename F::Frag b[NT][4];
+    typename F::Frag b[F::kParts][NT][4];
     float sc[NT][UPB];
     uint4 w[NT][2];                                  // the lane's chunks h and h + 2 of a row
 #pragma unroll
@@ -220,25 +220,21 @@ __global__ __launch_bounds__(kThreads, kPerCu) void packed_gemm_kernel(const Gem
 #pragma unroll
       for (int u = 0; u < UPB; ++u) sc[t][u] = *reinterpret_cast<const float*>(wt + L::kW + (wave * UPB + u) * 256 + (t * 32 + l31) * 4);
     }
-    auto unpack = [&](int part) __attribute__((always_inline)) {
+    auto unpack = [&](int part, int f) __attribute__((always_inline)) { b[part][f / 4][f % 4] = F::unpack(w[f / 4][0], w[f / 4][1], part, f % 4); };
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) b[t][i] = F::unpack(w[t][0], w[t][1], part, i);
-    };
+    for (int f = 0; f < 4 * NT; ++f) unpack(0, f);
     const unsigned char* xt = smem + slot * L::kStage + l31 * ROWB;
     const int sz = F::swizzle(l31);
     slot = slot + 1 == L::kRing ? 0 : slot + 1;
     // Tiles one after another, (token tile, run, row tile).  While a tile's instructions run, the one before it is taken up in
     // float32: from the second instruction on, when the last one's result is there.  Where a unit spans both parts of a stage and the
-    // registers hold all tiles' accumulators, they are kept from part to part and taken up once.
+    // registers hold all tiles' accumulators, they are kept from part to part and taken up once; the next part's codes are unpacked meanwhile.
     constexpr int PER = NT * RUNS, TILES = MT * PER;
     constexpr bool KEEP = F::kParts > 1 && UPB == 1;
     constexpr int ACCS = KEEP ? TILES : 2;
     typename F::Acc acc[ACCS];
 #pragma unroll
     for (int part = 0; part < F::kParts; ++part) {
-      unpack(part);
       typename F::Frag x[4];
       auto read_x = [&](int m, int i) __attribute__((always_inline)) {
         x[i] = *reinterpret_cast<const typename F::Frag*>(xt + m * 32 * ROWB + (F::chunk(part, i, h) ^ sz) * 16);
@@ -264,9 +260,10 @@ __global__ __launch_bounds__(kThreads, kPerCu) void packed_gemm_kernel(const Gem
         const int m = j / PER, u = j / NT % RUNS, t = j % NT;
 #pragma unroll
         for (int i = 0; i < SPU; ++i) {
-          acc[j % ACCS] = F::mul(x[u * SPU + i], b[t][u * SPU + i], i == 0 && !(KEEP && part) ? typename F::Acc{} : acc[j % ACCS]);
+          acc[j % ACCS] = F::mul(x[u * SPU + i], b[part][t][u * SPU + i], i == 0 && !(KEEP && part) ? typename F::Acc{} : acc[j % ACCS]);
           if (t == NT - 1 && m + 1 < MT) read_x(m + 1, u * SPU + i);
           __builtin_amdgcn_sched_barrier(0);
+          if (part + 1 < F::kParts && (j * SPU + i) % (MT * RUNS * SPU / 4) == 0) unpack(part + 1, (j * SPU + i) / (MT * RUNS * SPU / 4));
           if (j > 0 && taken) {
             if (SPU == 4) take(j - 1, i == 0 ? 0 : i - 1, i == 0 ? 0 : i == 3 ? 4 : i);
             else if (SPU == 2) take(j - 1, i, i == 0 ? 1 : 4);
