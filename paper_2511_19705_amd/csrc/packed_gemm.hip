@@ -1,6 +1,6 @@
 // Products with packed 4-bit weights for many tokens: tiles on the 32x32 matrix instructions.
 //   y[t][o] = sum over units of s[o][unit] (sx[t][unit]) sum_{c in unit} q[o][c] x[t][c]
-// A workgroup of four waves owns 32 MT tokens x 128 NT rows of the weight; a wave owns all its tokens and 32 NT of the rows.  The
+// A workgroup of four or eight waves owns 32 MT tokens; a wave owns all of them and 32 NT rows of the weight.  The
 // activations of 128 columns go to LDS asynchronously, a stage ahead of the one being multiplied; the weights, which no other
 // wave of the workgroup needs, go to registers, 4 bits a weight, and are unpacked there once for the 32 MT tokens.
 #include "cafeq_common.hpp"
@@ -13,7 +13,8 @@ namespace {
 using i32x16 = __attribute__((__vector_size__(16 * sizeof(int)))) int;
 using f32x16 = __attribute__((__vector_size__(16 * sizeof(float)))) float;
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
+// waves of a workgroup: eight where a stage of four leaves room for no more than two of its kind on a compute unit
+constexpr int tile_waves(bool i8, int mt, int nt) { return mt * nt >= (i8 ? 8 : 4) ? 8 : 4; }
 
 struct GemmArgs {
   const uint8_t* packed;
@@ -33,7 +34,7 @@ struct GemmArgs {
   int tok_tiles, row_tiles;  // tiles of the workgroups
   int whole;              // tiles that one workgroup takes whole; of the others every one goes to `split` of them
   int split;
-  float* part;            // [tile - whole][split][32 MT * 128 NT], in the accumulators' order
+  float* part;            // [tile - whole][split][tokens x rows of a tile], in the accumulators' order
 };
 
 // tile number -> (token tile, row tile): token tiles of a group of eight side by side, so that workgroups that run together share
@@ -80,16 +81,17 @@ template <> struct Form<false> {
 // What a workgroup holds in LDS: a ring of stages, as many as leave room for a second workgroup on the compute unit.  All of a stage --
 // activations, weights, scales -- is requested asynchronously, so that a wave knows how many requests follow those of a stage (weights
 // loaded to registers instead cost the compiler's waits: 3584 x 14336 and 64 tokens 28 us against 20, 1024 tokens in bfloat16 209 against 143).
-constexpr int kPerCu = 2;
 template <bool I8, int MT, int NT, int FG, bool SX>
 struct Lds {
+  static constexpr int kWaves = tile_waves(I8, MT, NT), kThreads = 64 * kWaves;
   static constexpr int kTok = 32 * MT, kUnits = kBlockK / FG;
   static constexpr int kX = kTok * Form<I8>::kRowBytes;              // a stage: activations,
-  static constexpr int kW = 128 * NT * 64;                           // weights,
+  static constexpr int kW = 32 * NT * kWaves * 64;                           // weights,
   static constexpr int kSw = kWaves * kUnits * 256;                  // their scales [wave][unit][64],
   static constexpr int kSx = SX ? kUnits * kThreads * 4 : 0;         // scales of the activations [unit][256]
   static constexpr int kStage = kX + kW + kSw + kSx;
-  static constexpr int kRing = 80 * 1024 / kStage < 2 ? 2 : 80 * 1024 / kStage > 6 ? 6 : 80 * 1024 / kStage;
+  static constexpr int kRoom = 160 * 1024 / (8 / kWaves);           // eight waves a compute unit
+  static constexpr int kRing = kRoom / kStage < 2 ? 2 : kRoom / kStage > 6 ? 6 : kRoom / kStage;
   static constexpr int kBytes = kRing * kStage;
   // requests of a wave for a stage
   static constexpr int kDma = kX / 16 / kThreads + kW / 16 / kThreads + kUnits * (SX ? 2 : 1);
@@ -105,9 +107,10 @@ __device__ __forceinline__ void lds_dma4(uint32_t to, uint32_t off, const void* 
 }
 
 template <bool I8, int MT, int NT, int FG, bool SX>
-__global__ __launch_bounds__(kThreads, kPerCu) void packed_gemm_kernel(const GemmArgs a) {
+__global__ __launch_bounds__(64 * tile_waves(I8, MT, NT), 2) void packed_gemm_kernel(const GemmArgs a) {
   using F = Form<I8>;
   using L = Lds<I8, MT, NT, FG, SX>;
+  constexpr int kWaves = L::kWaves, kThreads = L::kThreads;
   constexpr int ROWB = F::kRowBytes, CH = ROWB / 16;
   constexpr int NDMA = L::kX / 16 / kThreads;        // requests of a thread and stage
   constexpr int UPB = kBlockK / FG;                 // units of a stage
@@ -162,9 +165,9 @@ __global__ __launch_bounds__(kThreads, kPerCu) void packed_gemm_kernel(const Gem
     dma(plane, kb, slot);
     const uint32_t to = uint32_t(slot * L::kStage + L::kX);
 #pragma unroll
-    for (int i = 0; i < 2 * NT; ++i) {       // the workgroup's tiles of 16 rows 4 i + wave, as they lie in memory
-      const int64_t tile = min(int64_t(rt) * (TROWS / kRowTile) + 4 * i + wave, a.p.row_tiles - 1);
-      lds_dma16(to + uint32_t(4 * i + wave) * 1024u, uint32_t(lane) * 16u, a.packed + (tile * nkb + kb) * 1024);
+    for (int i = 0; i < 2 * NT; ++i) {       // the workgroup's tiles of 16 rows kWaves i + wave, as they lie in memory
+      const int64_t tile = min(int64_t(rt) * (TROWS / kRowTile) + kWaves * i + wave, a.p.row_tiles - 1);
+      lds_dma16(to + uint32_t(kWaves * i + wave) * 1024u, uint32_t(lane) * 16u, a.packed + (tile * nkb + kb) * 1024);
     }
 #pragma unroll
     for (int u = 0; u < UPB; ++u) {
@@ -302,14 +305,14 @@ __global__ __launch_bounds__(kThreads, kPerCu) void packed_gemm_kernel(const Gem
 }
 
 // the pieces of a tile in order, to Y
-__global__ __launch_bounds__(256) void packed_join_kernel(const GemmArgs a, int mt, int nt, bool per_token, float unit) {
-  const int size = 32 * mt * 32 * nt * kWaves;
+__global__ __launch_bounds__(256) void packed_join_kernel(const GemmArgs a, int mt, int nt, int waves, bool per_token, float unit) {
+  const int size = 32 * mt * 32 * nt * waves;
   const int tile = blockIdx.y, e = blockIdx.x * 256 + threadIdx.x;
   int tt, rt;
   place(a.whole + tile, a, &tt, &rt);
   const int lane = e & 63, r = e >> 6 & 15, at = e >> 10, t = at % nt, m = at / nt % mt, wave = at / nt / mt;   // as the kernel leaves them
   const int64_t tok = int64_t(tt) * 32 * mt + m * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-  const int64_t row = int64_t(rt) * (32 * nt * kWaves) + (wave * nt + t) * 32 + (lane & 31);
+  const int64_t row = int64_t(rt) * (32 * nt * waves) + (wave * nt + t) * 32 + (lane & 31);
   if (tok >= a.n || row >= a.p.rows) return;
   const float* p = a.part + int64_t(tile) * a.split * size + e;
   float v = 0.f;
@@ -334,7 +337,7 @@ __global__ __launch_bounds__(256) void split_planes_of_x_kernel(const float* __r
 }
 
 struct Plan {
-  int mt, nt, tok_tiles, row_tiles, whole, split;
+  int mt, nt, waves, tok_tiles, row_tiles, whole, split;
   size_t part_at, bytes;
 };
 
@@ -350,16 +353,16 @@ constexpr TileCost kTilesBf16[] = {{1, 1, 0.62f, 0.88f}, {2, 1, 0.83f, 1.27f}, {
 Plan make_plan(int x_type, int64_t n, const PackedShape& p) {
   Plan best{};
   double least = 1e30;
-  const int cus = device_cu_count(), slots = kPerCu * cus;
+  const int cus = device_cu_count();
   const int stages = int(p.kblocks) * (x_type == CAFEQ_F32 ? 3 : 1);
   auto consider = [&](const TileCost& c) {
-    const int trows = 32 * c.nt * kWaves;
+    const int waves = tile_waves(x_type == CAFEQ_I8, c.mt, c.nt), trows = 32 * c.nt * waves, slots = 8 / waves * cus;
     const int64_t tok_tiles = (n + 32 * c.mt - 1) / (32 * c.mt), row_tiles = (p.rows + trows - 1) / trows, tiles = tok_tiles * row_tiles;
     const int64_t whole = tiles / slots * slots, rest = tiles - whole;
-    // pieces of so many stages, two workgroups a compute unit at a time; 1.5 us to begin and end one
+    // pieces of so many stages, eight waves a compute unit at a time; 1.5 us to begin and end one
     auto run = [&](int64_t pieces, int64_t depth) {
       const int64_t left = pieces % slots;
-      return double(pieces / slots) * (double(depth) * c.paired + 1.5) + (left ? double(depth) * (left > cus ? c.paired : c.alone) + 1.5 : 0.0);
+      return double(pieces / slots) * (double(depth) * c.paired + 1.5) + (left ? double(depth) * (left > cus || waves == 8 ? c.paired : c.alone) + 1.5 : 0.0);
     };
     for (int64_t split = 1; split == 1 || (split <= stages / 2 && rest * split <= 4 * slots); ++split) {
       const double per = run(whole, stages) + run(rest * split, (stages + split - 1) / split);
@@ -367,7 +370,7 @@ Plan make_plan(int x_type, int64_t n, const PackedShape& p) {
       const double t = per + join;
       if (t < least) {
         least = t;
-        best.mt = c.mt; best.nt = c.nt; best.tok_tiles = int(tok_tiles); best.row_tiles = int(row_tiles);
+        best.mt = c.mt; best.nt = c.nt; best.waves = waves; best.tok_tiles = int(tok_tiles); best.row_tiles = int(row_tiles);
         best.split = int(split); best.whole = int(split == 1 ? tiles : whole);
         best.bytes = split == 1 ? 0 : size_t(rest * split) * (32 * c.mt * trows * 4);
       }
@@ -389,7 +392,7 @@ int launch_one(const GemmArgs& a, unsigned nwg, hipStream_t st) {
     static const bool ok = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
     if (!ok) return CAFEQ_ERR_LAUNCH;
   }
-  hipLaunchKernelGGL(kern, dim3(nwg), dim3(kThreads), lds, st, a);
+  hipLaunchKernelGGL(kern, dim3(nwg), dim3(Lds<I8, MT, NT, FG, SX>::kThreads), lds, st, a);
   CAFEQ_CHECK_LAUNCH();
   return CAFEQ_OK;
 }
@@ -441,8 +444,8 @@ int launch_packed_gemm(const PackedCall& c, void* ws, hipStream_t st) {
   }
   if (rc) return rc;
   if (rest) {
-    const int size = 32 * g.mt * 32 * g.nt * kWaves;
-    hipLaunchKernelGGL(packed_join_kernel, dim3(size / 256, rest), dim3(256), 0, st, a, g.mt, g.nt, i8 && !sx, code_unit(i8));
+    const int size = 32 * g.mt * 32 * g.nt * g.waves;
+    hipLaunchKernelGGL(packed_join_kernel, dim3(size / 256, rest), dim3(256), 0, st, a, g.mt, g.nt, g.waves, i8 && !sx, code_unit(i8));
     CAFEQ_CHECK_LAUNCH();
   }
   return CAFEQ_OK;
