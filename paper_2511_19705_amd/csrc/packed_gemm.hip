@@ -1,8 +1,11 @@
 // Products with packed 4-bit weights for many tokens: tiles on the 32x32 matrix instructions.
 //   y[t][o] = sum over units of s[o][unit] (sx[t][unit]) sum_{c in unit} q[o][c] x[t][c]
-// A workgroup of four or eight waves owns 32 MT tokens; a wave owns all of them and 32 NT rows of the weight.  The
-// activations of 128 columns go to LDS asynchronously, a stage ahead of the one being multiplied; the weights, which no other
-// wave of the workgroup needs, go to registers, 4 bits a weight, and are unpacked there once for the 32 MT tokens.
+// A workgroup of four or eight waves owns 32 MT tokens; a wave owns all of them and 32 NT rows of the weight.  A stage is 128 columns:
+// activations, packed weights and scales go to a ring in LDS asynchronously, up to five stages ahead; a wave unpacks its rows' codes once for all
+// the tokens.  Bound by the vector instructions that unpack codes and take a unit's sums up in float32 (conversion, multiply-add), beside the
+// matrix instructions: 4608 x 36864, 4096 tokens of 8 bits, a scale each: 684 us, 2.03 POP/s (vector issue 72 % of the cycles, matrix pipe
+// 50 %); 14336 x 3584, 512 tokens in bfloat16 59 us, 890 TFLOP/s.  Between those and few tokens by the weights' stream: 36864 x 4608, 32 tokens
+// 26 us, 3.4 TB/s.
 #include "cafeq_common.hpp"
 #include "cafeq_internal.hpp"
 #include "packed.hpp"
@@ -78,7 +81,7 @@ template <> struct Form<false> {
   static __device__ __forceinline__ Acc mul(const Frag& x, const Frag& b, const Acc& c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, b, c, 0, 0, 0); }
 };
 
-// What a workgroup holds in LDS: a ring of stages, as many as leave room for a second workgroup on the compute unit.  All of a stage --
+// What a workgroup holds in LDS: a ring of stages, as many as leave room for eight waves on the compute unit.  All of a stage --
 // activations, weights, scales -- is requested asynchronously, so that a wave knows how many requests follow those of a stage (weights
 // loaded to registers instead cost the compiler's waits: 3584 x 14336 and 64 tokens 28 us against 20, 1024 tokens in bfloat16 209 against 143).
 template <bool I8, int MT, int NT, int FG, bool SX>
@@ -86,11 +89,11 @@ struct Lds {
   static constexpr int kWaves = tile_waves(I8, MT, NT), kThreads = 64 * kWaves;
   static constexpr int kTok = 32 * MT, kUnits = kBlockK / FG;
   static constexpr int kX = kTok * Form<I8>::kRowBytes;              // a stage: activations,
-  static constexpr int kW = 32 * NT * kWaves * 64;                           // weights,
+  static constexpr int kW = 32 * NT * kWaves * 64;                   // weights,
   static constexpr int kSw = kWaves * kUnits * 256;                  // their scales [wave][unit][64],
-  static constexpr int kSx = SX ? kUnits * kThreads * 4 : 0;         // scales of the activations [unit][256]
+  static constexpr int kSx = SX ? kUnits * kThreads * 4 : 0;         // scales of the activations [unit][threads]
   static constexpr int kStage = kX + kW + kSw + kSx;
-  static constexpr int kRoom = 160 * 1024 / (8 / kWaves);           // eight waves a compute unit
+  static constexpr int kRoom = 160 * 1024 / (8 / kWaves);            // eight waves a compute unit
   static constexpr int kRing = kRoom / kStage < 2 ? 2 : kRoom / kStage > 6 ? 6 : kRoom / kStage;
   static constexpr int kBytes = kRing * kStage;
   // requests of a wave for a stage
@@ -304,7 +307,7 @@ __global__ __launch_bounds__(64 * tile_waves(I8, MT, NT), 2) void packed_gemm_ke
     }
 }
 
-// the pieces of a tile in order, to Y
+// The pieces of a tile in order, to Y: 32 tiles of 128 x 512 in 8 pieces each, 67 MB of partial sums, 19 us (3.5 TB/s).
 __global__ __launch_bounds__(256) void packed_join_kernel(const GemmArgs a, int mt, int nt, int waves, bool per_token, float unit) {
   const int size = 32 * mt * 32 * nt * waves;
   const int tile = blockIdx.y, e = blockIdx.x * 256 + threadIdx.x;
@@ -320,7 +323,7 @@ __global__ __launch_bounds__(256) void packed_join_kernel(const GemmArgs a, int 
   store_y(a.y, a.ydtype, tok * a.ldy + row, v * ((per_token ? a.xscales[tok] : 1.f) * unit));
 }
 
-// float32 activations as three planes of bfloat16, the small parts first: hi + mid + lo exactly
+// float32 activations as three planes of bfloat16, the small parts first: hi + mid + lo exactly (bound by memory, 10 bytes an activation)
 __global__ __launch_bounds__(256) void split_planes_of_x_kernel(const float* __restrict__ x, int64_t ldx, int64_t n, int64_t cols, uint16_t* __restrict__ out) {
   const int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x, per = cols / 8;
   if (id >= n * per) return;

@@ -12,7 +12,8 @@
 namespace cafeq {
 namespace {
 
-// One thread a lane's 16 bytes: row tile, 128 columns, lane.
+// One thread a lane's 16 bytes: row tile, 128 columns, lane.  Run once for a weight: 36864 x 4608 70 us (3.7 TB/s; a lane's reads of eight codes
+// lie a row apart).
 __global__ __launch_bounds__(256) void pack_kernel(const int8_t* __restrict__ codes, const float* __restrict__ scales, PackedShape p,
                                                    uint8_t* __restrict__ packed) {
   const int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x;
@@ -45,7 +46,8 @@ __global__ __launch_bounds__(256) void pack_kernel(const int8_t* __restrict__ co
 // through LDS in order.  v_mfma 16x16: A the codes (16 rows), B the activations (16 tokens): a lane has four rows of one token, whose
 // scales are one 16-byte load.  Sums start anew every FG columns (the common divisor of both groups and 128) and are taken up in
 // float32 with their scales.  A wave requests U blocks at once (weights, activations, scales) before it multiplies the first: with few
-// tokens nothing but the bytes in flight counts.
+// tokens nothing but the bytes in flight counts.  One token of 8 bits, weights from memory: 36864 x 4608 17.2 us (5.2 TB/s), 3584 x 14336
+// 8.0; in bfloat16 22.0 and 9.5; 16 tokens of 8 bits 22.7 and 14.2 (every row tile reads their activations from L2).
 template <class X, int TT, int OT, int FG>
 __global__ __launch_bounds__(1024) void packed_small_kernel(const PackedCall a) {
   extern __shared__ float red[];
