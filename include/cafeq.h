@@ -224,7 +224,7 @@ int cafeq_infer_single(const float* X, int n, int64_t ldx, const cafeq_xform* xf
  * asked for.  A group of zeros has scale 0 and codes 0; one that holds an infinity or a NaN has codes 0 and that
  * magnitude as its scale, so that whatever reads it is not finite.  n = 0 does nothing; n up to 2^21, d up to 65536.
  * xf NULL: any d, strides and alignments (rows that start at multiples of 16 bytes with d a multiple of 8 are
- * faster); sum may be x or residual itself.  With xf: k in {32, 64, 128, 256}, nb*k == d, rep == 1; rows of x, residual,
+ * faster); sum may be x or residual itself, element by element, and overlap them in no other way.  With xf: k in {32, 64, 128, 256}, nb*k == d, rep == 1; rows of x, residual,
  * sum and values start at multiples of 16 bytes (as do codes and Tinv), sum may overlap neither x nor residual
  * (CAFEQ_ERR_INVALID_ARG), and ws holds cafeq_norm_workspace_bytes(n, d, xf, group) bytes, 16-byte aligned (group < 0: no
  * codes). */

@@ -623,9 +623,16 @@ bool group_in_tile(int64_t group) { return group <= kOut && (group & (group - 1)
 // 1 / rms of the rows, where a launch of its own forms them
 size_t norms_bytes(int64_t n) { return n > kFuseTok ? align_up(size_t(n) * sizeof(float), 256) : 0; }
 
-bool overlaps(const void* a, int64_t bytes_a, const void* b, int64_t bytes_b) {
+// Whether rows of d elements at a (leading dimension lda) and at b share memory.  Of rows with one leading dimension only their columns decide:
+// slices side by side of one buffer do not overlap.
+bool overlaps(const void* a, int64_t lda, const void* b, int64_t ldb, int64_t n, int64_t d, int size) {
+  if (!a || !b || n < 1) return false;
   const auto p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
-  return a && b && p < q + uint64_t(bytes_b) && q < p + uint64_t(bytes_a);
+  const uint64_t row = uint64_t(d) * size, sa = uint64_t(n - 1) * lda * size + row, sb = uint64_t(n - 1) * ldb * size + row;
+  if (p >= q + sb || q >= p + sa) return false;
+  if (n == 1 || lda != ldb) return true;
+  const uint64_t ld = uint64_t(lda) * size, off = (p > q ? p - q : q - p) % ld;
+  return off < row || off > ld - row;
 }
 
 }  // namespace
@@ -672,12 +679,13 @@ int cafeq_norm_quantize(const cafeq_activations* in, int64_t n, int64_t d, const
       return CAFEQ_ERR_BAD_ALIGN;
     if (!ws && cafeq_norm_workspace_bytes(n, d, xf, codes ? group : -1)) return CAFEQ_ERR_WORKSPACE;
     if (!aligned(ws, 16)) return CAFEQ_ERR_BAD_ALIGN;
-    // x and residual are read a second time, after the sum has been written
-    const int64_t span = size * ((n - 1) * in->lds + d);
-    if (n > 0 && in->sum && (overlaps(in->sum, span, in->x, size * ((n - 1) * in->ldx + d)) ||
-                             (in->residual && overlaps(in->sum, span, in->residual, size * ((n - 1) * in->ldr + d)))))
-      return CAFEQ_ERR_INVALID_ARG;
   }
+  // the sum's elements may take the place of those that they come from, where nothing reads these again; no other overlap
+  auto bad_sum = [&](const void* from, int64_t ld) {
+    if (!xf && in->sum == from && in->lds == ld) return false;
+    return overlaps(in->sum, in->lds, from, ld, n, d, size);
+  };
+  if (in->sum && (bad_sum(in->x, in->ldx) || bad_sum(in->residual, in->ldr))) return CAFEQ_ERR_INVALID_ARG;
   if (n == 0) return CAFEQ_OK;
   hipStream_t st = static_cast<hipStream_t>(stream);
   RowArgs a{};

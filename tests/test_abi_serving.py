@@ -48,6 +48,10 @@ def test_norm_refuses(cq):
     assert _norm(cq, gain=FAKE + 2) == ALIGN
     assert _norm(cq, scales=FAKE + 2) == ALIGN
     assert _norm(cq, n=0) == 0
+    assert _norm(cq, sum=FAKE + 4) == INVALID            # neither x itself nor apart from it
+    assert _norm(cq, sum=FAKE, lds=68) == INVALID
+    assert _norm(cq, residual=FAKE + 65536, sum=FAKE + 65536 + 128) == INVALID
+    assert _norm(cq, ldx=96, sum=FAKE + 96, lds=96) == INVALID   # columns that reach into x's
 
 
 def test_norm_with_a_transform_refuses(cq):

@@ -288,3 +288,14 @@ def test_rows_past_two_gigabytes(env, k):
     rest = torch.ones(n, dtype=torch.bool, device="cuda:0")
     rest[at] = False
     assert not o.codes[rest].any() and not o.scales[rest].any()
+
+
+@pytest.mark.parametrize("k", [0, 32])
+def test_operands_side_by_side_in_one_buffer(env, k):
+    torch, cafeq = env
+    buf = torch.randn((5, 3 * 64), device="cuda:0")
+    x, r, total = buf[:, :64], buf[:, 64:128], buf[:, 128:]
+    P = torch.linalg.qr(torch.randn((2, 32, 32)))[0].contiguous().cuda() if k else None
+    want = cafeq.norm_quantize(x.clone(), residual=r.clone(), Tinv=P, group=32)
+    got = cafeq.norm_quantize(x, residual=r, Tinv=P, group=32, sum_out=total)
+    assert torch.equal(total, want.sum) and torch.equal(got.codes, want.codes) and torch.equal(got.scales, want.scales)
