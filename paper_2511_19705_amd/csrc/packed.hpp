@@ -103,7 +103,9 @@ __device__ __forceinline__ void store_y(void* y, int dtype, int64_t at, float v)
 }
 
 // The forms of the activations.  Chunk: 16 consecutive columns of a token (a lane's share of 64) as loaded; Form: as the matrix
-// instructions take them; mul: 64 columns of 16 rows times 16 tokens onto acc, the weights' two dwords of the same columns.
+// instructions take them; mul: 64 columns of 16 rows times 16 tokens onto acc, the weights' two dwords of the same columns; mul_in: of the
+// lanes for which `in` is set only.  The others have codes of zero where the products are integers; where they are floats it is the
+// activations that are zero there: an infinity times a code of zero would be no number.
 struct XI8 {
   static constexpr bool kScaled = true;
   static constexpr int kSize = 1;
@@ -117,6 +119,9 @@ struct XI8 {
   static __device__ __forceinline__ void mul(Acc& acc, uint32_t w0, uint32_t w1, const Form& f) {
     const i32x4 a = {int(low16(w0)), int(high16(w0)), int(low16(w1)), int(high16(w1))};
     acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, f, acc, 0, 0, 0);
+  }
+  static __device__ __forceinline__ void mul_in(Acc& acc, uint32_t w0, uint32_t w1, const Form& f, bool in) {
+    mul(acc, in ? w0 : 0u, in ? w1 : 0u, f);
   }
   static __device__ __forceinline__ float value(const Acc& acc, int r) { return float(acc[r]); }
 };
@@ -138,6 +143,12 @@ struct XBf16 {
   static __device__ __forceinline__ void mul(Acc& acc, uint32_t w0, uint32_t w1, const Form& f) {
     acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_codes(w0), f.v[0], acc, 0, 0, 0);
     acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_codes(w1), f.v[1], acc, 0, 0, 0);
+  }
+  static __device__ __forceinline__ void mul_in(Acc& acc, uint32_t w0, uint32_t w1, const Form& f, bool in) {
+    Form g;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) g.v[e] = in ? f.v[e] : bf16x8_t{};
+    mul(acc, w0, w1, g);
   }
   static __device__ __forceinline__ float value(const Acc& acc, int r) { return acc[r]; }
 };
@@ -180,6 +191,14 @@ struct XF32 {
 #pragma unroll
       for (int s = 2; s >= 0; --s) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, f.v[e][s], acc, 0, 0, 0);   // the small parts first
     }
+  }
+  static __device__ __forceinline__ void mul_in(Acc& acc, uint32_t w0, uint32_t w1, const Form& f, bool in) {
+    Form g;
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int s = 0; s < 3; ++s) g.v[e][s] = in ? f.v[e][s] : bf16x8_t{};
+    mul(acc, w0, w1, g);
   }
   static __device__ __forceinline__ float value(const Acc& acc, int r) { return acc[r]; }
 };

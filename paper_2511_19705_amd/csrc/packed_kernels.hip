@@ -136,9 +136,7 @@ __global__ __launch_bounds__(1024) void packed_small_kernel(const PackedCall a) 
               } else if constexpr (FG == 64) {
                 X::mul(acc, u ? c.z : c.x, u ? c.w : c.y, xf[u]);
               } else {
-                // 32 of 64 columns: the codes of the other lanes as zeros
-                const uint32_t keep = (kq >> 1) == (u & 1) ? 0xFFFFFFFFu : 0u;
-                X::mul(acc, (u >> 1 ? c.z : c.x) & keep, (u >> 1 ? c.w : c.y) & keep, xf[u >> 1]);
+                X::mul_in(acc, u >> 1 ? c.z : c.x, u >> 1 ? c.w : c.y, xf[u >> 1], (kq >> 1) == (u & 1));   // 32 of 64 columns
               }
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
