@@ -222,7 +222,8 @@ int cafeq_infer_single(const float* X, int n, int64_t ldx, const cafeq_xform* xf
  * (group 0: one a row; else a multiple of 32 that divides d); both NULL: no codes.  values (may be NULL if codes
  * is not; float32 or bfloat16, leading dimension ldv): fl(q*scale), the values the codes stand for, or z where no codes are
  * asked for.  A group of zeros has scale 0 and codes 0; one that holds an infinity or a NaN has codes 0 and that
- * magnitude as its scale, so that whatever reads it is not finite.  n = 0 does nothing; n up to 2^21, d up to 65536.
+ * magnitude as its scale, so that whatever reads it is not finite.  n = 0 does nothing; n up to 2^21, d up to 65536;
+ * of a single row no leading dimension matters beyond being d at least.
  * xf NULL: any d, strides and alignments (rows that start at multiples of 16 bytes with d a multiple of 8 are
  * faster); sum may be x or residual itself, element by element, and overlap them in no other way.  With xf: k in {32, 64, 128, 256}, nb*k == d, rep == 1; rows of x, residual,
  * sum and values start at multiples of 16 bytes (as do codes and Tinv), sum may overlap neither x nor residual
@@ -259,7 +260,8 @@ int cafeq_pack_nibbles(const int8_t* codes, const float* scales, int64_t out, in
  *                           else a multiple of 32 that divides in)
  * Y float32 or bfloat16 [n][out], leading dimension ldy >= out.  Sums over a group are exact integers with CAFEQ_I8 and
  * float32 otherwise (no activation is rounded); groups are added in float32 in a fixed order, and one rounding leads to Y.
- * Y must not overlap X.  n = 0 does nothing; n up to 2^19, ldx up to 2^24.  ws: cafeq_infer_packed_workspace_bytes() bytes (0 for few tokens), 16-byte aligned. */
+ * Y must not overlap X.  n = 0 does nothing; n up to 2^19, ldx up to 2^24
+ * (a single row: any ldx >= in).  ws: cafeq_infer_packed_workspace_bytes() bytes (0 for few tokens), 16-byte aligned. */
 size_t cafeq_infer_packed_workspace_bytes(int x_type, int64_t n, int64_t out, int64_t in, int64_t group);
 int cafeq_infer_packed(const void* X, int x_type, int64_t n, int64_t ldx, const float* xscales, int64_t xgroup,
                        const void* packed, int64_t out, int64_t in, int64_t group, void* Y, int y_dtype,

@@ -658,6 +658,12 @@ int cafeq_norm_quantize(const cafeq_activations* in, int64_t n, int64_t d, const
   if (!codes && !values) return CAFEQ_ERR_INVALID_ARG;
   if (n < 0 || d < 1 || in->ldx < d || (in->residual && in->ldr < d) || (in->sum && in->lds < d) || (values && ldv < d))
     return CAFEQ_ERR_BAD_SHAPE;
+  cafeq_activations single;
+  if (n == 1) {   // a single row has no next one: as if it lay alone
+    single = *in;
+    single.ldx = single.ldr = single.lds = ldv = d;
+    in = &single;
+  }
   if (d > kMaxRow || n > (int64_t(1) << 21)) return CAFEQ_ERR_UNSUPPORTED;   // a launch's threads stay below 2^32
   int64_t g = 0;
   if (codes) {

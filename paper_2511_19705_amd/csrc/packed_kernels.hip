@@ -248,6 +248,7 @@ int cafeq_infer_packed(const void* X, int x_type, int64_t n, int64_t ldx, const 
   const int rc = packed_shape(out, in, group, &p);
   if (rc) return rc;
   if (n < 0 || ldx < in || ldy < out) return CAFEQ_ERR_BAD_SHAPE;
+  if (n == 1) ldx = in;   // a single row has no next one
   const int64_t gx = x_type != CAFEQ_I8 || xgroup == 0 ? in : xgroup;
   if (gx < 32 || gx % 32 != 0 || in % gx != 0) return CAFEQ_ERR_BAD_SHAPE;
   const int size = x_type == CAFEQ_F32 ? 4 : x_type == CAFEQ_BF16 ? 2 : 1;
