@@ -7,6 +7,7 @@ There is no fallback: if the library is missing or a call fails, an exception is
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import NamedTuple, Optional
 
@@ -609,6 +610,11 @@ class PackedWeight(NamedTuple):
     group: int
 
 
+@functools.lru_cache(maxsize=None)
+def _packed_bytes(rows, cols, group):
+    return int(lib.cafeq_packed_bytes(rows, cols, group))
+
+
 def pack_nibbles(codes, scales, group):
     """Codes of up to 4 bits and their scales (AXIS_COL, as rtn_quantize returns them) packed for infer_packed."""
     if codes.dim() != 2:
@@ -616,7 +622,7 @@ def pack_nibbles(codes, scales, group):
     dev = torch._C._cuda_getDevice()
     rows, cols = codes.shape
     pcodes = _operand(codes, dev, torch.int8, (rows, cols), "codes")
-    nbytes = lib.cafeq_packed_bytes(rows, cols, group)
+    nbytes = _packed_bytes(rows, cols, group)
     if nbytes == 0:
         raise CafeqError("cannot pack codes of this shape (columns and group must be multiples of 32, the group a divisor)")
     pscales = _operand(scales, dev, torch.float32, _scale_shape(rows, cols, group, AXIS_COL), "scales")
@@ -639,6 +645,8 @@ def infer_packed(X, weight, xscales=None, xgroup=0, dtype=torch.float32, out=Non
     n, d = X.shape
     if d != cols or data.get_device() != dev:
         raise CafeqError("X must have the columns (%d) and the device of the weight" % cols)
+    if data.numel() != (_packed_bytes(rows, cols, group) or -1) or data.dtype is not torch.uint8 or not data.is_contiguous():
+        raise CafeqError("weight: its buffer is not one that pack_nibbles made for %d x %d with groups of %d" % (rows, cols, group))
     ps = None
     if kind == I8:
         if xscales is None or xgroup < 0 or (xgroup and d % xgroup):

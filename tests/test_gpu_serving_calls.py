@@ -1,4 +1,4 @@
-"""What the serving calls take beside their sizes: the leading dimension of a single row."""
+"""What the serving calls take and refuse beside their sizes: the leading dimension of a single row, packed buffers of another weight."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -57,3 +57,18 @@ def test_norms_of_one_row_take_any_leading_dimension(env, dtype, k):
     assert got.sum is sv
     for a, b in zip(want, got):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("n", [1, 4])
+def test_packed_buffers_that_do_not_fit_are_refused(env, n):
+    torch, cafeq = env
+    packed = _packed(torch, cafeq, 40, 64)
+    x = torch.ones((n, 64), device="cuda:0")
+    full = packed.data
+    for data in (full[:-16], full[:0], torch.cat((full, full)), full.view(torch.float32), torch.cat((full, full))[::2]):
+        with pytest.raises(cafeq.CafeqError):
+            cafeq.infer_packed(x, packed._replace(data=data))
+    for rows, group in ((100, 32), (40, 0), (40, 48), (-1, 32)):
+        with pytest.raises(cafeq.CafeqError):
+            cafeq.infer_packed(x, packed._replace(rows=rows, group=group))
+    assert torch.equal(cafeq.infer_packed(x, packed._replace(data=full.clone())), cafeq.infer_packed(x, packed))
