@@ -616,7 +616,8 @@ def _packed_bytes(rows, cols, group):
 
 
 def pack_nibbles(codes, scales, group):
-    """Codes of up to 4 bits and their scales (AXIS_COL, as rtn_quantize returns them) packed for infer_packed."""
+    """Codes of up to 4 bits and their scales (AXIS_COL, as rtn_quantize returns them) packed for infer_packed.  Codes outside [-8, 7] are refused;
+    seeing them takes a read of all codes and a wait, once a weight (none while a graph is captured, which must not wait)."""
     if codes.dim() != 2:
         raise CafeqError("codes must be a 2-D tensor")
     dev = torch._C._cuda_getDevice()
@@ -626,6 +627,10 @@ def pack_nibbles(codes, scales, group):
     if nbytes == 0:
         raise CafeqError("cannot pack codes of this shape (columns and group must be multiples of 32, the group a divisor)")
     pscales = _operand(scales, dev, torch.float32, _scale_shape(rows, cols, group, AXIS_COL), "scales")
+    if not torch.cuda.is_current_stream_capturing():
+        low, high = torch.stack(torch.aminmax(codes)).tolist()
+        if low < -8 or high > 7:
+            raise CafeqError("codes must lie in [-8, 7], these in [%d, %d]: more than 4 bits?" % (low, high))
     buf = torch.empty(nbytes, dtype=torch.uint8, device=codes.device)
     _check(lib.cafeq_pack_nibbles(pcodes, pscales, rows, cols, group, buf.data_ptr(), _stream()))
     return PackedWeight(buf, rows, cols, group)

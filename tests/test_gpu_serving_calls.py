@@ -1,4 +1,5 @@
-"""What the serving calls take and refuse beside their sizes: the leading dimension of a single row, packed buffers of another weight."""
+"""What the serving calls take and refuse beside their sizes: the leading dimension of a single row, packed buffers of another weight, codes of
+more than four bits."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -72,3 +73,35 @@ def test_packed_buffers_that_do_not_fit_are_refused(env, n):
         with pytest.raises(cafeq.CafeqError):
             cafeq.infer_packed(x, packed._replace(rows=rows, group=group))
     assert torch.equal(cafeq.infer_packed(x, packed._replace(data=full.clone())), cafeq.infer_packed(x, packed))
+
+
+@pytest.mark.parametrize("bits", [5, 8])
+def test_codes_of_more_than_four_bits_are_refused(env, bits):
+    torch, cafeq = env
+    W = torch.randn((40, 64), device="cuda:0")
+    codes, scales, _ = cafeq.rtn_quantize(W, bits, 32)
+    with pytest.raises(cafeq.CafeqError):
+        cafeq.pack_nibbles(codes, scales, 32)
+    codes, scales, _ = cafeq.rtn_quantize(W, 4, 32)
+    for low, high, good in ((-8, 7, True), (-9, 0, False), (0, 8, False)):
+        codes[3, 5], codes[39, 63] = low, high
+        if good:
+            cafeq.pack_nibbles(codes, scales, 32)
+        else:
+            with pytest.raises(cafeq.CafeqError):
+                cafeq.pack_nibbles(codes, scales, 32)
+
+
+def test_packing_in_a_captured_graph(env):
+    torch, cafeq = env
+    codes, scales, _ = cafeq.rtn_quantize(torch.randn((40, 64), device="cuda:0"), 4, 32)
+    cafeq.pack_nibbles(codes, scales, 32)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = cafeq.pack_nibbles(codes, scales, 32)
+    x = torch.randn((2, 64), device="cuda:0")
+    for _ in range(3):
+        codes.copy_(torch.randint(-8, 8, (40, 64), device="cuda:0", dtype=torch.int8))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(cafeq.infer_packed(x, held), cafeq.infer_packed(x, cafeq.pack_nibbles(codes, scales, 32)))
