@@ -650,7 +650,7 @@ def infer_packed(X, weight, xscales=None, xgroup=0, dtype=torch.float32, out=Non
     n, d = X.shape
     if d != cols or data.get_device() != dev:
         raise CafeqError("X must have the columns (%d) and the device of the weight" % cols)
-    if data.numel() != (_packed_bytes(rows, cols, group) or -1) or data.dtype is not torch.uint8 or not data.is_contiguous():
+    if data.numel() != _packed_bytes(rows, cols, group) or not data.is_contiguous():   # (of another type than bytes: at least as large)
         raise CafeqError("weight: its buffer is not one that pack_nibbles made for %d x %d with groups of %d" % (rows, cols, group))
     ps = None
     if kind == I8:
