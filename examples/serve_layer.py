@@ -53,7 +53,7 @@ def main(argv=None):
     ap.add_argument("--tokens", type=int, default=1)
     ap.add_argument("--k", type=int, default=128)
     ap.add_argument("--group", type=int, default=128)
-    ap.add_argument("--bits", type=int, default=4)
+    ap.add_argument("--bits", type=int, default=4, choices=(2, 3, 4))
     ap.add_argument("--steps", type=int, default=10)
     a = ap.parse_args(argv)
     gen = torch.Generator(device=DEVICE).manual_seed(0)

@@ -218,15 +218,17 @@ int cafeq_infer_single(const float* X, int n, int64_t ldx, const cafeq_xform* xf
  *   z[b*k + i] = sum_j Tinv[b][i][j] y[b*k + j]          (z = y where xf is NULL; only Tinv, k, nb of it are read)
  *   a = max |z| over a group, inv = min(fl(127 / a), FLT_MAX), q = rint(fl(z*inv)), scale = fl(a / 127)
  * x, residual, sum: float32 or bfloat16 (one type), leading dimensions in elements; sum (may be NULL) receives h, rounded
- * once; all arithmetic is float32 on the unrounded h.  codes int8 [n][d] dense, scales float32 [n][d/group]
+ * once; all arithmetic is float32 on the unrounded h (squares as they are: where a row's sum of them passes float32, its finite
+ * elements have y = 0; the transform rounds numbers of magnitude below 2^-110 to multiples of 2^-133).  codes int8 [n][d] dense,
+ * scales float32 [n][d/group]
  * (group 0: one a row; else a multiple of 32 that divides d); both NULL: no codes.  values (may be NULL if codes
  * is not; float32 or bfloat16, leading dimension ldv): fl(q*scale), the values the codes stand for, or z where no codes are
  * asked for.  A group of zeros has scale 0 and codes 0; one that holds an infinity or a NaN has codes 0 and that
  * magnitude as its scale, so that whatever reads it is not finite.  n = 0 does nothing; n up to 2^21, d up to 65536;
- * of a single row no leading dimension matters beyond being d at least.
+ * of a single row no leading dimension matters beyond being d at least.  codes, scales and values overlap no input.
  * xf NULL: any d, strides and alignments (rows that start at multiples of 16 bytes with d a multiple of 8 are
- * faster); sum may be x or residual itself, element by element, and overlap them in no other way.  With xf: k in {32, 64, 128, 256}, nb*k == d, rep == 1; rows of x, residual,
- * sum and values start at multiples of 16 bytes (as do codes and Tinv), sum may overlap neither x nor residual
+ * faster); sum may be x or residual itself, element by element, and overlap them in no other way.  With xf: k in {32, 64, 128, 256},
+ * nb*k == d, rep == 1; rows of x, residual, sum and values start at multiples of 16 bytes (as do codes and Tinv), sum may overlap neither x nor residual
  * (CAFEQ_ERR_INVALID_ARG), and ws holds cafeq_norm_workspace_bytes(n, d, xf, group) bytes, 16-byte aligned (group < 0: no
  * codes). */
 typedef struct {
@@ -258,8 +260,12 @@ int cafeq_pack_nibbles(const int8_t* codes, const float* scales, int64_t out, in
  *   CAFEQ_F32, CAFEQ_BF16   the activations (already through the transform); xscales NULL, xgroup ignored
  *   CAFEQ_I8                codes of cafeq_norm_quantize with their scales xscales [n][in/xgroup] (xgroup 0: one a token;
  *                           else a multiple of 32 that divides in)
- * Y float32 or bfloat16 [n][out], leading dimension ldy >= out.  Sums over a group are exact integers with CAFEQ_I8 and
- * float32 otherwise (no activation is rounded); groups are added in float32 in a fixed order, and one rounding leads to Y.
+ * Y float32 or bfloat16 [n][out], leading dimension ldy >= out.  A row is summed in units of 128 columns, or of 64 or 32 where a
+ * group is no multiple of more: a unit's sum is an exact integer with CAFEQ_I8 and float32 otherwise (no activation of magnitude
+ * 2^-110 or more is rounded, smaller float32 ones to multiples of 2^-133).  Units take their scales and are added in float32 in a
+ * fixed order, those of one group too, and one rounding leads to Y.  An infinite activation gives what the sum above gives; a
+ * scale that is not finite leaves nothing finite in its row, or its token.  With CAFEQ_I8 sums are held times 16: a result of
+ * 2^124 and more may come out infinite.
  * Y must not overlap X.  n = 0 does nothing; n up to 2^19, ldx up to 2^24
  * (a single row: any ldx >= in).  ws: cafeq_infer_packed_workspace_bytes() bytes (0 for few tokens), 16-byte aligned. */
 size_t cafeq_infer_packed_workspace_bytes(int x_type, int64_t n, int64_t out, int64_t in, int64_t group);

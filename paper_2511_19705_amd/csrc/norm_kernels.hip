@@ -374,7 +374,8 @@ constexpr int tile_waves(int k, bool few) { return few || k == 256 ? 2 : 4; }
 // norms itself: reading them costs it less than a launch.
 // Bound: few tokens the launch and reading Tinv (64 KB a workgroup at blocks of 128; one token of 4608 columns 6.8 us, of 3584 through
 // blocks of 256 9.3), many the vector instructions around the products (2048 x 4608, blocks of 128, sum, codes and values: 25 us after the 9 of
-// the norms).
+// the norms; groups that no tile holds, with z through memory and the row kernel after it, 10 us more).  Blocks of 64 of float32 rows, without their
+// norms: four waves a SIMD spill 16 registers.
 template <int K, int KW, class Tag, bool FUSED, int WAVES>
 __global__ __launch_bounds__(256 * KW, WAVES) void act_tile_kernel(const TileArgs t) {
   constexpr int YC = K > kOut ? K : kOut;              // columns of y that the outputs need

@@ -23,7 +23,7 @@ inline int packed_shape(int64_t out, int64_t in, int64_t group, PackedShape* p) 
   if (out < 1 || in < 32 || in % 32 != 0 || group < 0) return CAFEQ_ERR_BAD_SHAPE;
   const int64_t g = group == 0 ? in : group;
   if (g % 32 != 0 || in % g != 0) return CAFEQ_ERR_BAD_SHAPE;
-  if (in > 65536 || out > (int64_t(1) << 24)) return CAFEQ_ERR_UNSUPPORTED;   // integer sums of a group stay below 2^31
+  if (in > 65536 || out > (int64_t(1) << 24)) return CAFEQ_ERR_UNSUPPORTED;   // a row has at most 2048 units, as unit_group() needs
   p->rows = out;
   p->cols = in;
   p->group = g;
@@ -158,7 +158,7 @@ struct XF32 {
   static constexpr int kSize = 4;
   using Acc = f32x4;
   struct Chunk { float v[16]; };
-  struct Form { bf16x8_t v[2][3]; };   // three parts of every activation, hi + mid + lo exactly
+  struct Form { bf16x8_t v[2][3]; };   // three parts of every activation, hi + mid + lo exactly (down to bfloat16's 2^-133)
   static __device__ __forceinline__ Chunk load(const void* x, int at, bool in) {
     Chunk c;
     const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(x) + at);

@@ -5,7 +5,8 @@
 // the tokens.  Bound by the vector instructions that unpack codes and take a unit's sums up in float32 (conversion, multiply-add), beside the
 // matrix instructions: 4608 x 36864, 4096 tokens of 8 bits, a scale each: 684 us, 2.03 POP/s (vector issue 72 % of the cycles, matrix pipe
 // 50 %); 14336 x 3584, 512 tokens in bfloat16 59 us, 890 TFLOP/s.  Between those and few tokens by the weights' stream: 36864 x 4608, 32 tokens
-// 26 us, 3.4 TB/s.
+// of 8 bits, a scale each 29 us from memory, 3.0 TB/s (25 from the memory-side cache).  Shorter units and grouped scales take their sums up more often:
+// 36864 x 4608, 3000 tokens of 8 bits in groups of 128 / 64 / 32 621 / 765 / 1066 us, with a scale per group of the activations too 706 / 980 / 1549.
 #include "cafeq_common.hpp"
 #include "cafeq_internal.hpp"
 #include "packed.hpp"
@@ -344,7 +345,8 @@ struct Plan {
   size_t part_at, bytes;
 };
 
-// What a stage of a tile takes, in us: on a compute unit alone, and with a second workgroup there (groups of 128, 4608 columns, one or two
+// What a stage of a tile takes, in us: on a compute unit alone, and with a second workgroup there (units of 128 and one scale a token, whose costs stand
+// for those of shorter units and grouped scales too; 4608 columns, one or two
 // workgroups a compute unit and, of the larger tiles, thousands).
 struct TileCost { int mt, nt; float alone, paired; };
 constexpr TileCost kTilesI8[] = {{1, 1, 0.48f, 0.69f}, {2, 1, 0.64f, 0.92f}, {2, 2, 1.1f, 1.75f}, {4, 2, 1.8f, 2.9f}};

@@ -3,7 +3,7 @@
 // The packed copy holds the codes in the order in which a lane of the matrix instructions takes them (pack_kernel), and each
 // row tile's scales behind each other.  Codes reach the matrix cores as 16 q: a nibble in the upper half of a byte is its
 // signed value times 16, so that two masks and a shift unpack eight of them, and the result is multiplied by 1 / 16 (exact) at
-// the end.  With 8-bit activations the sums over a group are exact integers; with float32 ones the activations are taken in
+// the end.  With 8-bit activations the sums over a unit of at most 128 columns are exact integers; with float32 ones the activations are taken in
 // three bfloat16 parts, exactly.
 #include "cafeq_common.hpp"
 #include "cafeq_internal.hpp"
@@ -46,8 +46,9 @@ __global__ __launch_bounds__(256) void pack_kernel(const int8_t* __restrict__ co
 // through LDS in order.  v_mfma 16x16: A the codes (16 rows), B the activations (16 tokens): a lane has four rows of one token, whose
 // scales are one 16-byte load.  Sums start anew every FG columns (the common divisor of both groups and 128) and are taken up in
 // float32 with their scales.  A wave requests U blocks at once (weights, activations, scales) before it multiplies the first: with few
-// tokens nothing but the bytes in flight counts.  One token of 8 bits, weights from memory: 36864 x 4608 17.2 us (5.2 TB/s), 3584 x 14336
-// 8.0; in bfloat16 22.0 and 9.5; 16 tokens of 8 bits 22.7 and 14.2 (every row tile reads their activations from L2).
+// tokens nothing but the bytes in flight counts.  Weights from memory / from the memory-side cache of 256 MB, us: one token of 8 bits, 36864 x 4608
+// 22.0 / 17.0 (4.1 / 5.3 TB/s), 3584 x 14336 9.3 / 7.5; in bfloat16 28.0 / 21.2 and 11.5 / 9.2; 16 tokens of 8 bits 26.0 / 22.5 and 14.9 / 14.1 (every
+// row tile reads their activations from L2).  float32 67 and 23: every row tile splits its activations anew, and one token's fill one of 16 columns.
 template <class X, int TT, int OT, int FG>
 __global__ __launch_bounds__(1024) void packed_small_kernel(const PackedCall a) {
   extern __shared__ float red[];
