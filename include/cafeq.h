@@ -273,6 +273,110 @@ int cafeq_infer_packed(const void* X, int x_type, int64_t n, int64_t ldx, const 
                        const void* packed, int64_t out, int64_t in, int64_t group, void* Y, int y_dtype,
                        int64_t ldy, void* ws, void* stream);
 
+/* ---- Serving between the projections: positions, a cache in 8 bits, attention ------------------------
+ *
+ * What stands between a quantized layer's q, k, v products and its output product.  Rows of these calls are the new tokens of a
+ * batch of sequences behind each other: sequence i owns rows starts[i] .. starts[i+1] - 1 (starts int32 [sequences+1] in device
+ * memory, not decreasing, from 0 to n at most), and its new tokens are the last of its lengths[i] tokens.  Rows of no sequence are
+ * left as they are.  x[t][head][c] of q, k, v and results: leading dimensions ld (a token) and hs (a head) in elements, channels
+ * side by side, so that slices of one fused product can be given as they are.
+ *
+ * cafeq_rotate_heads: the norm of each head, and the positions, in one pass over queries and keys:
+ *   y = x (mean_c x_c^2 + eps)^-1/2 (gain_offset + gain_c)       (y = x where norm is 0; gain NULL: factor 1)
+ *   pairs (a, b) of the first `rot` channels -> amplitude (a cos w - b sin w, a sin w + b cos w), w = positions[t] freq[i],
+ *   pair i being channels (i, i + rot/2), or (2i, 2i + 1) with interleaved; the other channels stay y.
+ * freq: rot/2 float64 in radians a position; the angle is formed and reduced in float64 (float32 loses it at far positions), the
+ * rest is float32, one rounding to dtype (float32 or bfloat16).  positions int32 [n].  d even, up to 512; rot even, 0 .. d.
+ * Any strides and alignments (d, rot, ld and hs multiples of 8 with 16-byte aligned pointers are faster).  out may be x itself
+ * with the same strides, and overlaps no input otherwise.  Either part may be absent (x NULL).  n up to 2^21, heads up to 4096. */
+typedef struct {
+  const void* x;
+  void* out;
+  int64_t ldx, hsx, ldo, hso;
+  int32_t heads;
+  const float* gain;      /* [d] or NULL */
+} cafeq_heads;
+typedef struct {
+  int32_t dtype, d, rot, interleaved, norm;
+  float eps, gain_offset, amplitude;
+} cafeq_rotation;
+int cafeq_rotate_heads(const cafeq_rotation* cfg, const cafeq_heads* q, const cafeq_heads* k, int64_t n, const int32_t* positions,
+                       const double* freq, void* stream);
+
+/* A cache of keys and values in pages of `block` tokens.  Codes are int8 on the symmetric grid of 8 bits with one float32 scale for
+ * each page and head:
+ *   k [pages][heads][block][d]   kscale [pages][heads]        v [pages][heads][d][block]   vscale [pages][heads]
+ * (a channel's tokens of v side by side: the order in which the matrix instructions contract over tokens).  table
+ * [sequences][width]: the page of each block of a sequence (blocks behind its length: -1); lengths [sequences]: its tokens;
+ * refs [pages]: rows of the table that hold a page (0: free; used by reserve, reorder and compact only).  All device memory, owned by the
+ * caller; k and v 16-byte aligned.  d a multiple of 16 up to 256, block 16, 32, 64 or 128, pages * heads up to 2^31 - 1, heads up to 4096,
+ * width * block below 2^31, sequences up to 65536.  Numbers in device memory are not trusted with addresses: lengths beyond width * block count as
+ * that, and tokens whose page is outside [0, pages) are not read or written and are no keys. */
+typedef struct {
+  int8_t* k;
+  int8_t* v;
+  float* kscale;
+  float* vscale;
+  int32_t* table;
+  int32_t* lengths;
+  int32_t* refs;
+  int64_t pages;
+  int32_t sequences, width, heads, d, block;
+} cafeq_cache;
+
+/* New keys and values k, v [n][heads][d] (float32 or bfloat16) into the pages of their sequences, at the last starts[i+1] - starts[i]
+ * of the lengths[i] positions (lengths count the new tokens already, as cafeq_cache_reserve leaves them).  For each page, head and side
+ * with the new tokens' largest magnitude a:
+ *   s = fl(a / 127), or max(s_old, that) where the page holds earlier tokens of the sequence; scale = s
+ *   new codes q = clamp(rint(fl(x * min(fl(1 / s), FLT_MAX))), -127, 127);  earlier codes q <- rint(fl(q * fl(s_old / s))) if s > s_old
+ * so earlier tokens are rounded again, by half a step of the new scale at most, each time the scale grows.  Zeros only: s = 0, codes 0.
+ * A NaN or an infinity leaves that as the scale of its page and head and codes 0 in it, then and later: nothing that reads it is finite.
+ * Two sequences that append must not share the page they append to (cafeq_cache_reserve sees to that).  longest: an upper
+ * bound of the new tokens of a sequence (rows beyond it are not stored).  Rows start at multiples of 16 bytes.  n up to 2^24. */
+int cafeq_cache_append(const cafeq_cache* cache, const void* k, const void* v, int dtype, int64_t n, int64_t ldk, int64_t hsk,
+                       int64_t ldv, int64_t hsv, const int32_t* starts, int64_t longest, void* stream);
+
+/* Reads back what the codes stand for, fl(q * scale), rounded to dtype: k, v [n][heads][d] dense (16-byte aligned, either may be NULL);
+ * row starts[i] + j is position begin[i] + j of sequence i.  Positions outside [0, lengths[i]) and missing pages give zeros. */
+int cafeq_cache_values(const cafeq_cache* cache, const int32_t* begin, const int32_t* starts, int64_t n, void* k, void* v, int dtype,
+                       void* stream);
+
+/* Attention of the new tokens over the cache.  Row j of sequence i stands at position p = lengths[i] - (starts[i+1] - starts[i]) + j; query
+ * head h reads key head h / (heads_q / heads):
+ *   x_t = scale q . K_t, with softcap > 0: softcap tanh(x_t / softcap);  keys t: 0 <= t < lengths[i], t <= p if causal, t > p - window if window > 0
+ *   out = sum_t exp(x_t) V_t / sum_t exp(x_t),  lse = log sum_t exp(x_t)   (a row without keys: 0 and -inf)
+ * K, V: the codes times their scales.  q, out float32 or bfloat16 (dtype); lse float32 [n][heads_q] dense or NULL.  Queries of bfloat16 are
+ * taken exactly (magnitudes below 2^-28 of the row's largest to multiples of 2^-39 of it), probabilities rounded to 11 bits; with float32 both are taken in two
+ * parts of 11 bits.  Sums are float32 in a fixed order.  A row of q that holds a NaN or an infinity gives NaN.  A page and head of v with a scale below 2^-100 counts as zeros.
+ * Rows start at multiples of 16 bytes; out overlaps no input.  longest as in cafeq_cache_append (rows beyond it are left).
+ * heads_q a multiple of heads, up to 4096; n up to 2^24, n * heads_q below 2^31.  ws: cafeq_cache_attend_workspace_bytes() bytes (may be 0), 16-byte aligned. */
+typedef struct {
+  const void* q;
+  void* out;
+  float* lse;
+  int64_t n, ldq, hsq, ldo, hso, longest;
+  const int32_t* starts;
+  int32_t dtype, heads_q, causal, window;
+  float scale, softcap;
+} cafeq_attention;
+size_t cafeq_cache_attend_workspace_bytes(const cafeq_cache* cache, const cafeq_attention* a);
+int cafeq_cache_attend(const cafeq_cache* cache, const cafeq_attention* a, void* ws, void* stream);
+
+/* Pages.  All three enqueue everything, decide on the device and wait for nothing, so that they can be captured; nothing else may use
+ * the cache on another stream meanwhile.  ws: cafeq_cache_pages_workspace_bytes(cache) bytes, 16-byte aligned.
+ * reserve: room for starts[i+1] - starts[i] more tokens of each sequence.  Row by row the lowest free pages (refs 0) are taken: first, where the
+ *   sequence's last page is partly filled and refs of it exceed 1, one that the page is copied to and that takes its place, then
+ *   one for each new block.  lengths grow, refs follow.  positions (int32 [n] or NULL): the position of every new token.  missing
+ *   (int32 [1]): 0, or how many pages or table columns lack; then nothing is changed.
+ * reorder: row i takes over what row sources[i] held before the call (sources int32 [sequences], any value outside [0, sequences): nothing; the row's own number: it
+ *   stays).  The same source may be given several times: pages are shared, refs count their rows.  Pages that no row holds any more are free.
+ * compact: pages in use move to the lowest numbers (page by page in order, only those that have to), tables and refs with them; used (int32 [1]): how many there are. */
+size_t cafeq_cache_pages_workspace_bytes(const cafeq_cache* cache);
+int cafeq_cache_reserve(const cafeq_cache* cache, const int32_t* starts, int64_t n, int32_t* positions, int32_t* missing, void* ws,
+                        void* stream);
+int cafeq_cache_reorder(const cafeq_cache* cache, const int32_t* sources, void* ws, void* stream);
+int cafeq_cache_compact(const cafeq_cache* cache, int32_t* used, void* ws, void* stream);
+
 /* Z = W.blockdiag(X) or blockdiag(X).W with X = T (CAFEQ_SIDE_T) or Tinv
  * (CAFEQ_SIDE_TINV)  (paper Sec. 4.1 block-diagonal M; Sec. 4.2 U = W1 M, V = M^-1 W2).
  * Z: float32 [rows][cols] dense, must not alias W. */

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import os
 from typing import NamedTuple, Optional
 
@@ -31,6 +32,8 @@ EXPORTS = (
     "cafeq_infer_single", "cafeq_infer_workspace_bytes", "cafeq_set_launch_timing", "cafeq_rtn_quantize_static", "cafeq_prepared_bytes", "cafeq_prepare_weights",
     "cafeq_stream_read_probe", "cafeq_norm_quantize", "cafeq_norm_workspace_bytes", "cafeq_packed_bytes", "cafeq_pack_nibbles",
     "cafeq_infer_packed", "cafeq_infer_packed_workspace_bytes",
+    "cafeq_rotate_heads", "cafeq_cache_append", "cafeq_cache_values", "cafeq_cache_attend", "cafeq_cache_attend_workspace_bytes",
+    "cafeq_cache_reserve", "cafeq_cache_reorder", "cafeq_cache_compact", "cafeq_cache_pages_workspace_bytes",
 )
 
 
@@ -69,6 +72,29 @@ class Activations(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("sum", ctypes.c_void_p), ("ldx", ctypes.c_int64),
                 ("ldr", ctypes.c_int64), ("lds", ctypes.c_int64), ("dtype", ctypes.c_int32), ("norm", ctypes.c_int32),
                 ("gain", ctypes.c_void_p), ("gain_offset", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("hsx", ctypes.c_int64), ("ldo", ctypes.c_int64),
+                ("hso", ctypes.c_int64), ("heads", ctypes.c_int32), ("gain", ctypes.c_void_p)]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("d", ctypes.c_int32), ("rot", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("norm", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("gain_offset", ctypes.c_float), ("amplitude", ctypes.c_float)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("kscale", ctypes.c_void_p), ("vscale", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("lengths", ctypes.c_void_p), ("refs", ctypes.c_void_p), ("pages", ctypes.c_int64), ("sequences", ctypes.c_int32), ("width", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("d", ctypes.c_int32), ("block", ctypes.c_int32)]
+
+
+class Attention(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("n", ctypes.c_int64), ("ldq", ctypes.c_int64),
+                ("hsq", ctypes.c_int64), ("ldo", ctypes.c_int64), ("hso", ctypes.c_int64), ("longest", ctypes.c_int64), ("starts", ctypes.c_void_p),
+                ("dtype", ctypes.c_int32), ("heads_q", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("softcap", ctypes.c_float)]
 
 
 def _load():
@@ -126,6 +152,16 @@ def _load():
     lib.cafeq_pack_nibbles.argtypes = [vp, vp, i64, i64, i64, vp, vp]
     lib.cafeq_infer_packed.argtypes = [vp, i32, i64, i64, vp, i64, vp, i64, i64, i64, vp, i32, i64, vp, vp]
     lib.cafeq_infer_packed_workspace_bytes.argtypes = [i32, i64, i64, i64, i64]
+    cache = ctypes.POINTER(Cache)
+    lib.cafeq_rotate_heads.argtypes = [ctypes.POINTER(Rotation), ctypes.POINTER(Heads), ctypes.POINTER(Heads), i64, vp, vp, vp]
+    lib.cafeq_cache_append.argtypes = [cache, vp, vp, i32, i64, i64, i64, i64, i64, vp, i64, vp]
+    lib.cafeq_cache_values.argtypes = [cache, vp, vp, i64, vp, vp, i32, vp]
+    lib.cafeq_cache_attend.argtypes = [cache, ctypes.POINTER(Attention), vp, vp]
+    lib.cafeq_cache_attend_workspace_bytes.argtypes = [cache, ctypes.POINTER(Attention)]
+    lib.cafeq_cache_reserve.argtypes = [cache, vp, i64, vp, vp, vp, vp]
+    lib.cafeq_cache_reorder.argtypes = [cache, vp, vp, vp]
+    lib.cafeq_cache_compact.argtypes = [cache, vp, vp, vp]
+    lib.cafeq_cache_pages_workspace_bytes.argtypes = [cache]
     for n in EXPORTS[3:]:
         getattr(lib, n).restype = ctypes.c_size_t if n.endswith("_bytes") else i32
     return lib
@@ -679,3 +715,231 @@ def infer_packed(X, weight, xscales=None, xgroup=0, dtype=torch.float32, out=Non
         if rc:
             _check(rc)
     return out
+
+
+def rotary_frequencies(rot, base=10000.0, scaling="none", factor=1.0, trained=8192, low=1.0, high=32.0, device=None):
+    """(freq, amplitude) for rotate_heads: float64 [rot/2], base^(-2 i / rot) in radians a position, scaled for contexts `factor` times the
+    `trained` one:
+      none     as they are
+      linear   all divided by factor (positions between the trained ones)
+      base     base * factor^(rot / (rot - 2)): the highest frequency stays, the lowest is divided by factor
+      parts    a frequency that turns more than `high` times over the trained context stays, one of less than `low` turns is divided by factor,
+               linear in the turns between (arXiv 2309.00071, Sec. 3.2); amplitude 0.1 ln(factor) + 1 (its Sec. 3.4)"""
+    if rot < 0 or rot % 2 or not base > 0 or not factor > 0:
+        raise CafeqError("need an even number of turned channels, and base and factor above 0")
+    if scaling not in ("none", "linear", "base", "parts"):
+        raise CafeqError("scaling must be none, linear, base or parts")
+    if scaling == "parts" and (not trained > 0 or not high > low):
+        raise CafeqError("need a trained context above 0 and high above low")
+    exponent = torch.arange(0, rot, 2, dtype=torch.float64, device=device) / max(rot, 1)
+    if scaling == "base":
+        base = base * factor ** (rot / max(1, rot - 2))
+    freq = base ** -exponent
+    if scaling == "linear":
+        return freq / factor, 1.0
+    if scaling != "parts":
+        return freq, 1.0
+    turns = trained * freq / (2 * math.pi)
+    keep = ((turns - low) / (high - low)).clamp_(0.0, 1.0)
+    return freq * keep + freq / factor * (1.0 - keep), 0.1 * math.log(factor) + 1.0 if factor > 1 else 1.0
+
+
+def _head_rows(t, dev, what):
+    """(leading dimension, head stride) of a tensor [tokens][heads][d] with neighbouring channels on device number `dev`.  Strides that lead nowhere
+    (one token, one head) may be anything: they are given as those of a dense tensor."""
+    st = t.stride()
+    if len(st) != 3 or t.get_device() != dev or (st[2] != 1 and t.shape[2] > 1):
+        raise CafeqError("%s: need a tensor [tokens][heads][d] with unit channel stride on the current CUDA device" % what)
+    n, h, d = t.shape
+    hs = st[1] if h > 1 else d
+    return (st[0] if n > 1 else h * hs), hs
+
+
+def _part(x, out, gain, d, dev, what):
+    if x is None:
+        if out is not None or gain is not None:
+            raise CafeqError("%s is not given" % what)
+        return None, None
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    elif out.shape != x.shape or out.dtype is not x.dtype:
+        raise CafeqError("out_%s must have the shape and type of %s" % (what, what))
+    ldx, hsx = _head_rows(x, dev, what)
+    ldo, hso = _head_rows(out, dev, "out_" + what)
+    g = None if gain is None else _operand(gain, dev, torch.float32, (d,), "gain_" + what)
+    return Heads(x.data_ptr(), out.data_ptr(), ldx, hsx, ldo, hso, x.shape[1], g), out
+
+
+def rotate_heads(q, k, positions, freq, interleaved=False, norm=False, gain_q=None, gain_k=None, eps=1e-6, gain_offset=0.0, amplitude=1.0, out_q=None,
+                 out_k=None):
+    """cafeq_rotate_heads: root-mean-square norm of each head (norm=True; with gains) and rotary positions of the first 2 len(freq) channels.
+    q, k [n][heads][d] float32 or bfloat16 (either may be None), positions int32 [n], freq and amplitude as rotary_frequencies returns
+    them.  out_q, out_k: None (new tensors), or where the results go, which may be q and k themselves.  Returns (out_q, out_k)."""
+    x = q if q is not None else k
+    if x is None or x.dim() != 3:
+        raise CafeqError("need q or k, [n][heads][d]")
+    dev, kind = torch._C._cuda_getDevice(), _FLOATS.get(x.dtype)
+    if kind is None:
+        raise CafeqError("q and k must be float32 or bfloat16")
+    n, _, d = x.shape
+    if k is not None and (k.dim() != 3 or k.dtype is not x.dtype or k.shape[0] != n or k.shape[2] != d):
+        raise CafeqError("q and k must have the same type, tokens and channels")
+    pp = _operand(positions, dev, torch.int32, (n,), "positions")
+    pf = _operand(freq, dev, torch.float64, (freq.numel(),), "freq")
+    hq, out_q = _part(q, out_q, gain_q, d, dev, "q")
+    hk, out_k = _part(k, out_k, gain_k, d, dev, "k")
+    cfg = Rotation(kind, d, 2 * freq.numel(), 1 if interleaved else 0, 1 if norm else 0, eps, gain_offset, amplitude)
+    if n:
+        rc = lib.cafeq_rotate_heads(ctypes.byref(cfg), ctypes.byref(hq) if hq is not None else None, ctypes.byref(hk) if hk is not None else None, n, pp, pf,
+                                    torch._C._cuda_getCurrentRawStream(dev))
+        if rc:
+            _check(rc)
+    return out_q, out_k
+
+
+class KVCache(NamedTuple):
+    """A cache as cafeq.h describes it: codes and scales of keys and values, the page of each block of a sequence, tokens of a sequence, rows that
+    hold a page."""
+    k: torch.Tensor
+    v: torch.Tensor
+    kscale: torch.Tensor
+    vscale: torch.Tensor
+    table: torch.Tensor
+    lengths: torch.Tensor
+    refs: torch.Tensor
+
+
+def kv_cache(sequences, pages, heads, d, block=64, width=None, device=None):
+    """An empty cache: room for `sequences` rows of `width` blocks (all pages, if not given) over a pool of `pages` pages of `block` tokens."""
+    if block not in (16, 32, 64, 128) or d % 16 or not 16 <= d <= 256 or heads < 1 or pages < 1 or sequences < 0:
+        raise CafeqError("need blocks of 16, 32, 64 or 128 tokens and d a multiple of 16 up to 256")
+    device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+
+    def make(shape, dtype, value=0):
+        return torch.full(shape, value, dtype=dtype, device=device)
+
+    return KVCache(make((pages, heads, block, d), torch.int8), make((pages, heads, d, block), torch.int8), make((pages, heads), torch.float32),
+                   make((pages, heads), torch.float32), make((sequences, pages if width is None else width), torch.int32, -1),
+                   make((sequences,), torch.int32), make((pages,), torch.int32))
+
+
+def _cache(c, dev):
+    """Descriptor of a KVCache on device number `dev`."""
+    if len(c.k.shape) != 4 or len(c.table.shape) != 2:
+        raise CafeqError("cache: k must be [pages][heads][block][d], table [sequences][width]")
+    pages, heads, block, d = c.k.shape
+    rows, width = c.table.shape
+    i8, i32, f32 = torch.int8, torch.int32, torch.float32
+    return Cache(_operand(c.k, dev, i8, (pages, heads, block, d), "cache.k"), _operand(c.v, dev, i8, (pages, heads, d, block), "cache.v"),
+                 _operand(c.kscale, dev, f32, (pages, heads), "cache.kscale"), _operand(c.vscale, dev, f32, (pages, heads), "cache.vscale"),
+                 _operand(c.table, dev, i32, (rows, width), "cache.table"), _operand(c.lengths, dev, i32, (rows,), "cache.lengths"),
+                 _operand(c.refs, dev, i32, (pages,), "cache.refs"), pages, rows, width, heads, d, block)
+
+
+def _starts(t, rows, dev, what="starts"):
+    return _operand(t, dev, torch.int32, (rows + 1,), what)
+
+
+def cache_append(cache, k, v, starts, longest=None):
+    """cafeq_cache_append: new keys and values [n][heads][d] into the pages of their sequences, in 8 bits.  starts int32 [sequences + 1]: the rows
+    of each sequence, the last of its lengths' tokens; longest: an upper bound of a sequence's rows (n, if not given)."""
+    dev, kind = torch._C._cuda_getDevice(), _FLOATS.get(k.dtype)
+    if kind is None or v.dtype is not k.dtype:
+        raise CafeqError("k and v must be float32 or bfloat16, both the same")
+    c = _cache(cache, dev)
+    n = k.shape[0]
+    if k.shape != (n, c.heads, c.d) or v.shape != k.shape:
+        raise CafeqError("k and v must be [n][%d][%d]" % (c.heads, c.d))
+    (ldk, hsk), (ldv, hsv) = _head_rows(k, dev, "k"), _head_rows(v, dev, "v")
+    ps = _starts(starts, c.sequences, dev)
+    if n:
+        rc = lib.cafeq_cache_append(ctypes.byref(c), k.data_ptr(), v.data_ptr(), kind, n, ldk, hsk, ldv, hsv, ps, n if longest is None else longest,
+                                    torch._C._cuda_getCurrentRawStream(dev))
+        if rc:
+            _check(rc)
+
+
+def cache_values(cache, begin, starts, n, dtype=torch.float32):
+    """cafeq_cache_values: (k, v) [n][heads][d], the values of positions begin[i] .. of each sequence i in rows starts[i] .. starts[i + 1] - 1."""
+    dev, kind = torch._C._cuda_getDevice(), _FLOATS.get(dtype)
+    if kind is None:
+        raise CafeqError("dtype must be float32 or bfloat16")
+    c = _cache(cache, dev)
+    pb, ps = _operand(begin, dev, torch.int32, (c.sequences,), "begin"), _starts(starts, c.sequences, dev)
+    k, v = (torch.empty((n, c.heads, c.d), dtype=dtype, device=cache.k.device) for _ in range(2))
+    if n:
+        rc = lib.cafeq_cache_values(ctypes.byref(c), pb, ps, n, k.data_ptr(), v.data_ptr(), kind, torch._C._cuda_getCurrentRawStream(dev))
+        if rc:
+            _check(rc)
+    return k, v
+
+
+def cache_attend(cache, q, starts, longest=None, scale=None, softcap=0.0, window=0, causal=True, lse=False, out=None):
+    """cafeq_cache_attend: attention of new tokens q [n][heads_q][d] over the cache, which holds their keys and values already.  scale: d^-1/2 if
+    not given; softcap, window: 0 for none; starts, longest as in cache_append.  Returns out, or (out, lse [n][heads_q]) with lse=True."""
+    dev, kind = torch._C._cuda_getDevice(), _FLOATS.get(q.dtype)
+    if kind is None:
+        raise CafeqError("q must be float32 or bfloat16")
+    c = _cache(cache, dev)
+    if q.dim() != 3 or q.shape[2] != c.d or q.shape[1] < 1 or q.shape[1] % c.heads:
+        raise CafeqError("q must be [n][a multiple of %d][%d]" % (c.heads, c.d))
+    n, hq, d = q.shape
+    ldq, hsq = _head_rows(q, dev, "q")
+    if out is None:
+        out = torch.empty((n, hq, d), dtype=q.dtype, device=q.device)
+        ldo, hso = hq * d, d
+    else:
+        if out.shape != q.shape or out.dtype is not q.dtype:
+            raise CafeqError("out must have the shape and type of q")
+        ldo, hso = _head_rows(out, dev, "out")
+    sums = torch.empty((n, hq), dtype=torch.float32, device=q.device) if lse else None
+    a = Attention(q.data_ptr(), out.data_ptr(), None if sums is None else sums.data_ptr(), n, ldq, hsq, ldo, hso, n if longest is None else longest,
+                  _starts(starts, c.sequences, dev), kind, hq, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, softcap)
+    if n:
+        stream = torch._C._cuda_getCurrentRawStream(dev)
+        rc = lib.cafeq_cache_attend(ctypes.byref(c), ctypes.byref(a), None, stream)
+        if rc == _ERR_WORKSPACE:
+            # the buffer is of this call alone, so that streams share nothing
+            ws = q.new_empty(lib.cafeq_cache_attend_workspace_bytes(ctypes.byref(c), ctypes.byref(a)), dtype=torch.uint8)
+            rc = lib.cafeq_cache_attend(ctypes.byref(c), ctypes.byref(a), ws.data_ptr(), stream)
+        if rc:
+            _check(rc)
+    return (out, sums) if lse else out
+
+
+class Reserved(NamedTuple):
+    """What cache_reserve returns: the positions of the new tokens, and how many pages or table columns lack (0: there is room)."""
+    positions: torch.Tensor
+    missing: torch.Tensor
+
+
+def _pages_call(cache):
+    dev = torch._C._cuda_getDevice()
+    c = _cache(cache, dev)
+    ws = torch.empty(max(256, lib.cafeq_cache_pages_workspace_bytes(ctypes.byref(c))), dtype=torch.uint8, device=cache.k.device)
+    return dev, c, ws, torch._C._cuda_getCurrentRawStream(dev)
+
+
+def cache_reserve(cache, starts, n):
+    """cafeq_cache_reserve: room for starts[i + 1] - starts[i] more tokens of each sequence, n in all.  Nothing waits: a caller that cannot be
+    sure of room reads `missing` (one int32 on the device); where it is not 0 nothing has changed and positions hold nothing."""
+    dev, c, ws, stream = _pages_call(cache)
+    positions = torch.empty(n, dtype=torch.int32, device=cache.k.device)
+    missing = torch.empty(1, dtype=torch.int32, device=cache.k.device)
+    _check(lib.cafeq_cache_reserve(ctypes.byref(c), _starts(starts, c.sequences, dev), n, positions.data_ptr() if n else None, missing.data_ptr(), ws.data_ptr(),
+                                   stream))
+    return Reserved(positions, missing)
+
+
+def cache_reorder(cache, sources):
+    """cafeq_cache_reorder: row i takes over what row sources[i] held (int32 [sequences]; outside the rows: nothing, which lets its pages go)."""
+    dev, c, ws, stream = _pages_call(cache)
+    _check(lib.cafeq_cache_reorder(ctypes.byref(c), _operand(sources, dev, torch.int32, (c.sequences,), "sources"), ws.data_ptr(), stream))
+
+
+def cache_compact(cache):
+    """cafeq_cache_compact: pages in use move to the front of the pool.  Returns how many there are (int32 [1] on the device)."""
+    dev, c, ws, stream = _pages_call(cache)
+    used = torch.empty(1, dtype=torch.int32, device=cache.k.device)
+    _check(lib.cafeq_cache_compact(ctypes.byref(c), used.data_ptr(), ws.data_ptr(), stream))
+    return used
