@@ -1,0 +1,102 @@
+// Attention over the 8-bit cache: what its kernels share.
+//
+// Products run on the 16-bit matrix instructions with codes as float16 (exact) and transposed: S^T = K Q^T, out^T = V^T P^T.  A column of the
+// result is a query row, so that a lane holds scores of one row only, and the scores as they leave the first product are, rounded, what the
+// second one takes: nothing moves between lanes.
+//
+// A page's scale of v, mant 2^exp, goes into the exponent: with y = x + exp (x the score in units of log2) and M the largest y so far, rounded up, less 14,
+//   p = 2^(y - M) <= 2^14,   out = sum p mant c_v / sum p 2^-exp.
+// What is rounded to float16, p mant (to 11 bits down to 2^-28 of the largest), so is weighed as it counts in the result, however scales differ from page to page; and exp - M is a whole
+// number, so that the exponent's argument takes one rounding, in proportion to itself.
+#pragma once
+#include "cache.hpp"
+
+namespace cafeq {
+
+using half2_t = __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16;
+using half8_t = __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16;
+using f32x4_t = __attribute__((__vector_size__(4 * sizeof(float)))) float;
+using f32x16_t = __attribute__((__vector_size__(16 * sizeof(float)))) float;
+
+constexpr float kNoKey = -1.7e38f;       // M before the first key
+constexpr float kTop = 14.f;              // log2 of the largest p
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kZeroScale = 0x1p-100f;  // pages of v below it hold zeros: their keys have weight, and no value
+
+// Four codes of a dword as float16: 1024 + (q + 128) put together as bits, less 1152; exact.  Five instructions.
+__device__ __forceinline__ void half_codes(uint32_t w, half2_t* h) {
+  const uint32_t u = w ^ 0x80808080u;
+  const half2_t bias = {_Float16(-1152.f), _Float16(-1152.f)};
+  h[0] = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) + bias;
+  h[1] = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) + bias;
+}
+__device__ __forceinline__ half8_t half_codes(uint32_t w0, uint32_t w1) {
+  union { half2_t h[4]; half8_t v; } f;
+  half_codes(w0, f.h);
+  half_codes(w1, f.h + 2);
+  return f.v;
+}
+
+// The rows of one tile and what of the keys they reach.  Row R of a sequence and key head is token R / rep, query head R % rep of the group.
+struct Reach {
+  int i, row0;         // sequence, its first row of q
+  int len, pos0;       // its tokens; position of its first row
+  int rows;            // rows of the sequence and key head that are computed
+  int lo, hi;          // keys that any row of the tile reaches
+};
+__device__ __forceinline__ int key_end(const cafeq_attention& a, int len, int pos) { return a.causal ? min(len, pos + 1) : len; }
+__device__ __forceinline__ int key_begin(const cafeq_attention& a, int pos) { return a.window > 0 ? max(0, pos - a.window + 1) : 0; }
+
+__device__ __forceinline__ Reach reach_of(const cafeq_cache& c, const cafeq_attention& a, int i, int rep, int first, int count) {
+  Reach r;
+  const RowRange rr = rows_of(a.starts, i, int(a.n));
+  r.i = i;
+  r.row0 = rr.lo;
+  r.len = tokens_of(c, i);
+  r.pos0 = r.len - (rr.hi - rr.lo);
+  r.rows = int(min(int64_t(rr.hi - rr.lo), a.longest)) * rep;
+  const int last = min(first + count, r.rows) - 1;
+  r.lo = key_begin(a, r.pos0 + first / rep);
+  r.hi = last < first ? 0 : key_end(a, r.len, r.pos0 + last / rep);
+  return r;
+}
+
+// A page's scale of v as mant 2^exp; inv = 2^-exp.  A scale that is no number is its own mantissa.
+struct ValueScale { float exp, mant, inv; bool zero; };
+__device__ __forceinline__ ValueScale value_scale(float vs) {
+  ValueScale s;
+  const uint32_t u = __float_as_uint(vs) & 0x7FFFFFFFu, e = u >> 23;
+  s.zero = vs < kZeroScale;
+  const bool plain = e < 255 && !s.zero;
+  s.exp = plain ? float(int(e) - 127) : 0.f;
+  s.mant = plain ? __uint_as_float((u & 0x7FFFFFu) | 0x3F800000u) : s.zero ? 0.f : vs;
+  s.inv = plain ? __uint_as_float((254u - e) << 23) : 1.f;
+  return s;
+}
+
+struct AttendPlan {
+  cafeq_cache c;
+  cafeq_attention a;
+  int rep;
+  int tiles;          // row tiles of a sequence
+  int splits, span;   // parts that the keys of a tile may be cut into, steps of 64 keys in each
+  int keep;           // rows of a tile that have room in the parts
+  float* sums;        // parts [sequence][tile][head][split][keep]: (M, sum of weights)
+  float* parts;       // and [keep][d]
+};
+
+// Four channels of a finished row: v in units of 2^M, divided by the sum of weights
+template <class Tag>
+__device__ __forceinline__ void store_row(const AttendPlan& p, const Reach& r, int R, int head, int ch, f32x4_t v, float M, float total) {
+  const int64_t row = r.row0 + R / p.rep;
+  const int h = head * p.rep + R % p.rep;
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  typename Tag::elem* y = static_cast<typename Tag::elem*>(p.a.out) + row * p.a.ldo + h * p.a.hso + ch;
+  if constexpr (Tag::dtype == CAFEQ_F32) *reinterpret_cast<f32x4_t*>(y) = v * inv;
+  else *reinterpret_cast<uint2*>(y) = make_uint2(bf16_bits(v[0] * inv, v[1] * inv), bf16_bits(v[2] * inv, v[3] * inv));
+  if (p.a.lse && ch == 0) p.a.lse[row * p.a.heads_q + h] = total == 0.f ? -INFINITY : (M + log2f(total)) * kLn2;
+}
+
+int launch_attend_few(const AttendPlan& p, hipStream_t st);
+
+}  // namespace cafeq

@@ -152,13 +152,14 @@ class Pool:
 
 
 def attend(torch, cache, q, starts, scale, softcap, window, causal):
-    """float64 (out, lse, weight, size) on q's device from a library cache: weight = sum_t p |V| (what errors of the weights are counted
-    in), size [n][heads_q] = the largest scale * sum_c |q K| over a row's keys (what errors of the scores are counted in)."""
+    """float64 (out, lse, weight, size, floor) on q's device from a library cache: weight = sum_t p |V| (what errors of the weights are counted
+    in), size [n][heads_q] = the largest scale * sum_c |q K| over a row's keys (what errors of the scores are counted in), floor = sum_t |c| over a
+    row's keys times their largest scale of v, c the codes (what weights too small for float16's 11 bits are counted in)."""
     n, hq, d = q.shape
     pages, heads, B, _ = cache.k.shape
     dev = q.device
     out = torch.full((n, hq, d), float("nan"), dtype=torch.float64, device=dev)
-    weight, lse = torch.zeros_like(out), torch.full((n, hq), float("nan"), dtype=torch.float64, device=dev)
+    weight, floor, lse = torch.zeros_like(out), torch.zeros_like(out), torch.full((n, hq), float("nan"), dtype=torch.float64, device=dev)
     size = torch.zeros_like(lse)
     width = cache.table.shape[1]
     for i in range(len(starts) - 1):
@@ -180,6 +181,9 @@ def attend(torch, cache, q, starts, scale, softcap, window, causal):
             K = (cache.k[page, h].double() * cache.kscale[page, h].double()[:, None, None]).reshape(-1, d)[:length]
             V = (cache.v[page, h].double().transpose(1, 2) * cache.vscale[page, h].double()[:, None, None]).reshape(-1, d)[:length]
             used = live.any(0)
+            codes = cache.v[page, h].double().transpose(1, 2).reshape(-1, d)[:length].abs()
+            vs = torch.where(live, cache.vscale[page, h].double().repeat_interleave(B)[None, :length], torch.zeros((), dtype=torch.float64, device=dev))
+            most = (live.double() @ codes) * (vs.amax(1, keepdim=True) if length else 0.0)
             K = torch.where(used[:, None], K, torch.zeros_like(K))
             V = torch.where(used[:, None], V, torch.zeros_like(V))
             for g in range(h * (hq // heads), (h + 1) * (hq // heads)):
@@ -194,4 +198,5 @@ def attend(torch, cache, q, starts, scale, softcap, window, causal):
                 out[lo:hi, g] = p @ V
                 weight[lo:hi, g] = p @ V.abs()
                 lse[lo:hi, g] = norm
-    return out, lse, weight, size
+                floor[lo:hi, g] = most
+    return out, lse, weight, size, floor

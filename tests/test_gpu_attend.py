@@ -6,8 +6,11 @@ taken in two parts of 11 bits that leave 2^-22 of it; with d products, in two pa
 (8 u: products with the scales, soft cap, the exponent's argument; the cap passes errors on at most as they are).  A weight exp(x - max) is
 therefore off by e = 2 (that bound with |x| <= size) + 4 u of itself, numerator and denominator, and rounded to 11 bits (2^-12) with bfloat16,
 in two parts (2^-22) with float32.  The sum over N keys adds N u.  With W = sum p |V|
-    |out - ref| <= (2 e + r + (N + 16) u) W + h |out|,     r = 2^-12 or 2^-22, h = 2^-8 for results of bfloat16
+    |out - ref| <= (2 e + r + (N + 16) u) W + h |out| + 2^-38 floor,     r = 2^-12 or 2^-22, h = 2^-8 for results of bfloat16
     |lse - ref| <= 2 e + (N + 16) u + 8 u |lse|
+Weights p mant < 2^15 (p 2^14 at most, M rounded up by less than 1) below 2^-14 are subnormal in float16 and off by 2^-25 at most each, in the
+numerator sum p mant c of out = sum p mant c / sum p 2^-exp; the denominator is above 2^13 2^-exp of the key with the largest y, and 2^exp <= vs:
+    2^-25 sum |c| / (2^13 2^-exp) <= 2^-38 sum |c| max vs     more for out, "floor" below
 and, errors being of either sign, 3e-6 (float32) or 2^-8 (bfloat16) of the 2-norm of W."""
 import math
 
@@ -57,13 +60,13 @@ def _starts(counts, lead=0):
 def _near(env, cache, q, starts, out, lse, scale=None, softcap=0.0, window=0, causal=True):
     torch = env[0]
     d = q.shape[2]
-    want, wlse, W, size = R.attend(torch, cache, q, starts, d ** -0.5 if scale is None else scale, softcap, window, causal)
+    want, wlse, W, size, floor = R.attend(torch, cache, q, starts, d ** -0.5 if scale is None else scale, softcap, window, causal)
     rows = slice(starts[0], starts[-1])
-    out, want, W, size, wlse = out[rows].double(), want[rows], W[rows], size[rows], wlse[rows]
+    out, want, W, size, wlse, floor = out[rows].double(), want[rows], W[rows], size[rows], wlse[rows], floor[rows]
     u, f32 = 2.0 ** -24, q.dtype == torch.float32
     N = int(cache.lengths.max())
     e = 2 * (((2 * d + 16) * u + 2.0 ** -22) * size) + 4 * u
-    tol = (2 * e + (2.0 ** -22 if f32 else 2.0 ** -12) + (N + 16) * u)[:, :, None] * W + (0 if f32 else 2.0 ** -8) * want.abs() + 1e-37
+    tol = (2 * e + (2.0 ** -22 if f32 else 2.0 ** -12) + (N + 16) * u)[:, :, None] * W + (0 if f32 else 2.0 ** -8) * want.abs() + 2.0 ** -38 * floor + 1e-37
     err = (out - want).abs()
     assert not torch.isnan(err).any()
     assert (err <= tol).all(), float((err / tol).max())
