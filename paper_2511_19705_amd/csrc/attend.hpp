@@ -37,6 +37,18 @@ __device__ __forceinline__ half8_t half_codes(uint32_t w0, uint32_t w1) {
   return f.v;
 }
 
+__device__ __forceinline__ half2_t to_half(float a, float b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(half2_t, __builtin_convertvector((f32x2{a, b}), f16x2));
+}
+// out tanh(z); for results of bfloat16 by the hardware's exponential, good to 2^-22 of `out`
+template <bool F32>
+__device__ __forceinline__ float capped(float z, float out) {
+  if constexpr (F32) return tanhf(z) * out;
+  else return out - 2.f * out * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.f * kLog2e * z));
+}
+
 // The rows of one tile and what of the keys they reach.  Row R of a sequence and key head is token R / rep, query head R % rep of the group.
 struct Reach {
   int i, row0;         // sequence, its first row of q
@@ -77,9 +89,9 @@ __device__ __forceinline__ ValueScale value_scale(float vs) {
 struct AttendPlan {
   cafeq_cache c;
   cafeq_attention a;
-  int rep;
+  int rep, shift;     // query heads of a key head; log2 of the block
   int tiles;          // row tiles of a sequence
-  int splits, span;   // parts that the keys of a tile may be cut into, steps of 64 keys in each
+  int splits, span;   // parts that the keys of a tile may be cut into, steps of 32 keys in each
   int keep;           // rows of a tile that have room in the parts
   float* sums;        // parts [sequence][tile][head][split][keep]: (M, sum of weights)
   float* parts;       // and [keep][d]

@@ -24,7 +24,7 @@ int check_attention(const cafeq_cache* c, const cafeq_attention* a) {
 
 // How the rows and keys are cut.  Sums and parts lie behind each other in the workspace.
 AttendPlan plan(const cafeq_cache& c, const cafeq_attention& a) {
-  AttendPlan p{c, a, a.heads_q / c.heads};
+  AttendPlan p{c, a, a.heads_q / c.heads, __builtin_ctz(unsigned(c.block))};
   p.a.longest = std::min(a.longest, a.n);
   const int64_t rows = p.a.longest * p.rep, room = int64_t(c.width) * c.block;
   p.tiles = int((rows + 15) / 16);
@@ -32,9 +32,16 @@ AttendPlan plan(const cafeq_cache& c, const cafeq_attention& a) {
   // keys that a tile may reach
   const int64_t keys = a.window > 0 && a.causal ? std::min(room, a.window + 16 + int64_t(128)) : room;
   const int64_t groups = int64_t(c.sequences) * p.tiles * c.heads;
-  const int64_t part = std::min<int64_t>(4096, std::max<int64_t>(512, keys * groups / 1024));
-  p.span = int((part + 63) / 64);
-  p.splits = int((keys + 64 * p.span - 1) / (64 * p.span));
+  // Two workgroups a compute unit at once, but none with less than 128 keys (a step a wave) or more than 2048 (lengths differ); half as long where
+  // that leaves few to choose from.  us with 128 / 256 / 512 keys: 512 of 4 heads of 256 11.3 / 13.6 / 14.8, 4096 12.0 / 13.7 / 18.2; 32768 of 8 heads with
+  // 256 / 512 / 1024 keys 36 / 31.5 / 33; 48 x 8192 of 8 heads with 1024 / 2048 / 4096 318 / 302 / 323; 32 x 4096 of 4 heads, two row tiles, with
+  // 1024 / 2048 60 / 76.
+  int64_t part = std::min<int64_t>(2048, std::max<int64_t>(128, keys * groups / 512));
+  while (part > 512 && keys * groups / part < 1024) part /= 2;
+  p.span = int((part + 31) / 32);
+  p.span = std::max<int>(p.span, int((keys + int64_t(32) * 65535 - 1) / (int64_t(32) * 65535)));      // a grid's second dimension
+  p.splits = int((keys + 32 * int64_t(p.span) - 1) / (32 * int64_t(p.span)));
+  if (p.c.heads % 8 && p.splits % 2 == 0) ++p.splits;      // so that sequences begin on different XCDs
   return p;
 }
 size_t sums_bytes(const AttendPlan& p) {

@@ -6,7 +6,7 @@
 namespace cafeq {
 
 constexpr int kCacheDMax = 256;
-constexpr int64_t kMaxSeqs = 65536, kMaxHeads = 4096;
+constexpr int64_t kMaxSeqs = 65535, kMaxHeads = 4096;
 
 inline int check_cache(const cafeq_cache* c) {
   if (!c || !c->k || !c->v || !c->kscale || !c->vscale || (c->sequences && (!c->table || !c->lengths))) return CAFEQ_ERR_INVALID_ARG;
