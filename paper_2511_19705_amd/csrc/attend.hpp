@@ -86,12 +86,31 @@ __device__ __forceinline__ ValueScale value_scale(float vs) {
   return s;
 }
 
+// Rows of q are taken times a power of two that brings the largest magnitude (its bits) to [2^14, 2^15): bfloat16 then is exact in float16 down to
+// 2^-28 of it.  unit: what a product's sum is times, next to the scale of k, in the score (in log2 without a soft cap)
+struct QueryScale { float up, unit; };
+__device__ __forceinline__ QueryScale query_scale(uint32_t bits, const cafeq_attention& a) {
+  const int e = max(-100, int(bits >> 23) - 127);
+  QueryScale s;
+  s.up = copysignf(bits ? __uint_as_float(uint32_t(127 + 14 - e) << 23) : 1.f, a.scale);      // a negative scale is q's
+  s.unit = bits >= 0x7F800000u ? NAN : bits ? ldexpf(fabsf(a.scale), e - 14) : 0.f;
+  if (a.softcap <= 0.f) s.unit *= kLog2e;
+  return s;
+}
+
+// Many rows: keys of a tile, tiles of 32 rows a wave; what registers and LDS hold
+constexpr int many_keys(int db) { return db > 2 ? 32 : 64; }
+constexpr int many_tiles(int dtype, int db) { return 1; }
+constexpr int many_waves(int dtype, int db) { return dtype == CAFEQ_F32 && db > 2 ? 1 : 2; }
+
 struct AttendPlan {
   cafeq_cache c;
   cafeq_attention a;
   int rep, shift;     // query heads of a key head; log2 of the block
+  int few_rows;       // sequences with up to so many rows are attend_few's, the others attend_many's
+  Units units;        // attend_many: row tiles of all sequences
   int tiles;          // row tiles of a sequence
-  int splits, span;   // parts that the keys of a tile may be cut into, steps of 32 keys in each
+  int splits, span;   // parts that the keys of a tile may be cut into, steps of 32 keys (attend_many: tiles of keys) in each
   int keep;           // rows of a tile that have room in the parts
   float* sums;        // parts [sequence][tile][head][split][keep]: (M, sum of weights)
   float* parts;       // and [keep][d]
@@ -110,5 +129,6 @@ __device__ __forceinline__ void store_row(const AttendPlan& p, const Reach& r, i
 }
 
 int launch_attend_few(const AttendPlan& p, hipStream_t st);
+int launch_attend_many(const AttendPlan& p, hipStream_t st);
 
 }  // namespace cafeq

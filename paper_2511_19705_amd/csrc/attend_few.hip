@@ -54,7 +54,7 @@ __global__ __launch_bounds__(kThreads, Tag::dtype == CAFEQ_F32 && DB == 4 ? 1 : 
     ventry[n] = table[min((guess + n * kStep + vrun) >> shift_b, c.width - 1)];
   }
   const Reach r = reach_of(c, a, i, p.rep, first, kTile);
-  if (first >= r.rows) return;
+  if (first >= r.rows || r.rows > p.few_rows) return;
   const int c0 = r.lo / kStep, c1 = max(c0, (r.hi + kStep - 1) / kStep), used = max(1, (c1 - c0 + p.span - 1) / p.span);
   if (split >= used) return;
   const int begin = c0 + split * p.span, end = min(c1, begin + p.span);
@@ -119,13 +119,11 @@ __global__ __launch_bounds__(kThreads, Tag::dtype == CAFEQ_F32 && DB == 4 ? 1 : 
     for (int e = 0; e < 8; ++e) bits = max(bits, __float_as_uint(v[e]) & 0x7FFFFFFFu);
 #pragma unroll
     for (int m = 1; m < 32; m <<= 1) bits = max(bits, uint32_t(__shfl_xor(int(bits), m)));
-    // the row's largest magnitude to [2^14, 2^15): bfloat16 then is exact in float16 down to 2^-28 of it
-    const int e = max(-100, int(bits >> 23) - 127);
-    const float up = bits ? __uint_as_float(uint32_t(127 + 14 - e) << 23) : 1.f;
+    const QueryScale qs = query_scale(bits, a);
     half8_t h, rest;
 #pragma unroll
     for (int j = 0; j < 8; j += 2) {
-      const float f0 = v[j] * up, f1 = v[j + 1] * up;
+      const float f0 = v[j] * qs.up, f1 = v[j + 1] * qs.up;
       const half2_t x2 = to_half(f0, f1);
       h[j] = x2[0];
       h[j + 1] = x2[1];
@@ -140,12 +138,7 @@ __global__ __launch_bounds__(kThreads, Tag::dtype == CAFEQ_F32 && DB == 4 ? 1 : 
       q_lds[at] = h;
       if constexpr (kF32) q_lds[DB * 2 * 64 + at] = rest;
     }
-    if (chunk == 0) {
-      // a product's sum times this, times the scale of k, is the score (in log2 without a soft cap)
-      float unit = bits ? ldexpf(a.scale, e - 14) : 0.f;
-      if (bits >= 0x7F800000u) unit = NAN;
-      unit_lds[rr] = a.softcap > 0.f ? unit : unit * kLog2e;
-    }
+    if (chunk == 0) unit_lds[rr] = qs.unit;
   }
   __syncthreads();
   const float unit = unit_lds[l16];
@@ -352,7 +345,7 @@ __global__ __launch_bounds__(kJoin) void attend_join_kernel(const AttendPlan p) 
   const int row = blockIdx.z, tid = threadIdx.x;
   const Reach r = reach_of(c, p.a, i, p.rep, first, kTile);
   const int c0 = r.lo / kStep, c1 = max(c0, (r.hi + kStep - 1) / kStep), used = (c1 - c0 + p.span - 1) / p.span;
-  if (first + row >= r.rows || used <= 1) return;
+  if (first + row >= r.rows || r.rows > p.few_rows || used <= 1) return;
   const int per = d / 4, groups = kJoin / per, group = tid / per, ch = (tid - group * per) * 4;
   const int64_t part = (int64_t(i) * p.splits * gridDim.x + x) * p.keep + row, step = int64_t(gridDim.x) * p.keep;
   // the largest M; then weights and values in units of it

@@ -22,11 +22,26 @@ int check_attention(const cafeq_cache* c, const cafeq_attention* a) {
   return CAFEQ_OK;
 }
 
-// How the rows and keys are cut.  Sums and parts lie behind each other in the workspace.
-AttendPlan plan(const cafeq_cache& c, const cafeq_attention& a) {
+constexpr int64_t kFewRows = 64;
+
+size_t sums_bytes(const AttendPlan& p, int64_t tiles) {
+  return p.splits > 1 ? align_up(size_t(tiles) * p.c.heads * p.splits * p.keep * 2 * sizeof(float), 256) : 0;
+}
+size_t parts_bytes(const AttendPlan& p, int64_t tiles) { return sums_bytes(p, tiles) / 2 * size_t(p.c.d); }
+
+// How rows and keys are cut.  Sequences with up to few_rows rows a key head go to attend_few, the others to attend_many; one launch where the bound on
+// their tokens, or a single sequence, leaves no doubt.
+struct AttendPlans {
+  bool few, many;
+  AttendPlan f, m;
+  int64_t few_tiles, many_tiles;
+  size_t few_sums, few_parts, many_sums, many_parts;
+  size_t bytes() const { return few_sums + few_parts + many_sums + many_parts; }
+};
+
+AttendPlan plan_few(const cafeq_cache& c, const cafeq_attention& a, int64_t rows, int64_t room) {
   AttendPlan p{c, a, a.heads_q / c.heads, __builtin_ctz(unsigned(c.block))};
-  p.a.longest = std::min(a.longest, a.n);
-  const int64_t rows = p.a.longest * p.rep, room = int64_t(c.width) * c.block;
+  p.few_rows = int(std::min<int64_t>(rows, INT32_MAX));
   p.tiles = int((rows + 15) / 16);
   p.keep = int(std::min<int64_t>(16, rows));
   // keys that a tile may reach
@@ -44,10 +59,43 @@ AttendPlan plan(const cafeq_cache& c, const cafeq_attention& a) {
   if (p.c.heads % 8 && p.splits % 2 == 0) ++p.splits;      // so that sequences begin on different XCDs
   return p;
 }
-size_t sums_bytes(const AttendPlan& p) {
-  return align_up(size_t(p.c.sequences) * p.tiles * p.c.heads * p.splits * p.keep * 2 * sizeof(float), 256);
+
+AttendPlan plan_many(const cafeq_cache& c, const cafeq_attention& a, int64_t few_rows, int64_t room) {
+  AttendPlan p{c, a, a.heads_q / c.heads, __builtin_ctz(unsigned(c.block))};
+  const int db = (c.d + 63) / 64, tile = 128 * many_tiles(a.dtype, db), kt = many_keys(db);
+  p.few_rows = int(few_rows);
+  p.units = Units{p.rep, tile, 1};
+  p.keep = tile;
+  const int64_t keys = a.window > 0 && a.causal ? std::min(room, a.window + tile / p.rep + int64_t(2 * kt)) : room;
+  const int64_t groups = p.units.count(a.n, c.sequences) * c.heads;
+  // two workgroups a compute unit, none with less than 512 keys
+  const int64_t want = std::min((512 + groups - 1) / groups, (keys + 511) / 512);
+  p.span = int((keys + want * kt - 1) / (want * kt));
+  p.splits = int((keys + int64_t(p.span) * kt - 1) / (int64_t(p.span) * kt));
+  return p;
 }
-size_t plan_bytes(const AttendPlan& p) { return p.splits > 1 ? sums_bytes(p) + sums_bytes(p) / 2 * size_t(p.c.d) : 0; }
+
+AttendPlans plan(const cafeq_cache& c, const cafeq_attention& given) {
+  AttendPlans s{};
+  cafeq_attention a = given;
+  a.longest = std::min(a.longest, a.n);
+  const int64_t rep = a.heads_q / c.heads, rows = a.longest * rep, room = int64_t(c.width) * c.block;
+  s.many = rows > kFewRows;
+  s.few = !s.many || c.sequences > 1;
+  if (s.few) {
+    s.f = plan_few(c, a, std::min(rows, kFewRows), room);
+    s.few_tiles = int64_t(c.sequences) * s.f.tiles;
+    s.few_sums = sums_bytes(s.f, s.few_tiles);
+    s.few_parts = parts_bytes(s.f, s.few_tiles);
+  }
+  if (s.many) {
+    s.m = plan_many(c, a, s.few ? kFewRows : 0, room);
+    s.many_tiles = s.m.units.count(a.n, c.sequences);
+    s.many_sums = sums_bytes(s.m, s.many_tiles);
+    s.many_parts = parts_bytes(s.m, s.many_tiles);
+  }
+  return s;
+}
 
 }  // namespace
 }  // namespace cafeq
@@ -58,7 +106,7 @@ extern "C" {
 
 size_t cafeq_cache_attend_workspace_bytes(const cafeq_cache* cache, const cafeq_attention* a) {
   if (check_attention(cache, a) || a->n == 0 || a->longest == 0 || cache->sequences == 0) return 0;
-  return plan_bytes(plan(*cache, *a));
+  return plan(*cache, *a).bytes();
 }
 
 int cafeq_cache_attend(const cafeq_cache* cache, const cafeq_attention* a, void* ws, void* stream) {
@@ -66,13 +114,20 @@ int cafeq_cache_attend(const cafeq_cache* cache, const cafeq_attention* a, void*
   if (rc) return rc;
   if (!aligned_to(ws, 16)) return CAFEQ_ERR_BAD_ALIGN;
   if (a->n == 0 || a->longest == 0 || cache->sequences == 0) return CAFEQ_OK;
-  AttendPlan p = plan(*cache, *a);
-  if (plan_bytes(p)) {
-    if (!ws) return CAFEQ_ERR_WORKSPACE;
-    p.sums = static_cast<float*>(ws);
-    p.parts = p.sums + sums_bytes(p) / sizeof(float);
+  AttendPlans s = plan(*cache, *a);
+  if (s.bytes() && !ws) return CAFEQ_ERR_WORKSPACE;
+  char* at = static_cast<char*>(ws);
+  s.f.sums = reinterpret_cast<float*>(at);
+  s.f.parts = reinterpret_cast<float*>(at + s.few_sums);
+  at += s.few_sums + s.few_parts;
+  s.m.sums = reinterpret_cast<float*>(at);
+  s.m.parts = reinterpret_cast<float*>(at + s.many_sums);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (s.many) {
+    const int rc2 = launch_attend_many(s.m, st);
+    if (rc2) return rc2;
   }
-  return launch_attend_few(p, static_cast<hipStream_t>(stream));
+  return s.few ? launch_attend_few(s.f, st) : CAFEQ_OK;
 }
 
 }  // extern "C"

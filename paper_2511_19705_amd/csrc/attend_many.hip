@@ -1,0 +1,397 @@
+// Attention of many new tokens a sequence over the 8-bit cache: prompts, and chunks of them.
+#include "attend.hpp"
+#include "cafeq_internal.hpp"
+
+namespace cafeq {
+namespace {
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+
+__device__ __forceinline__ float other_half(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float lane_value(float v, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); }
+
+// A workgroup: 128 QT rows, 32 QT a wave, over a part of the keys, in tiles of KT.  A tile's codes are read once, become float16 on their way to LDS
+// and are what all waves multiply: v_mfma 32x32x16, S^T = K Q^T with the rows of q in registers, then out^T = V^T P^T.  Lane l holds row l % 32,
+// and of 32 keys those with key / 4 % 2 = l / 32: results i of a product are keys 8 (i / 4) + 4 (l / 32) + i % 4, weights 8 u .. 8 u + 7 what it gives to step u of
+// the second product.  LDS: K as [16 channels][half][key], V as [16 keys][half][channel] of eight float16 each, a place of 16 bytes
+// behind every run so that lanes that write side by side hit different banks.  Two buffers: the next tile's codes are on their way while this one is multiplied.
+template <class Tag, int DB, bool EXACT, int QT>
+__global__ __launch_bounds__(kThreads, many_waves(Tag::dtype, DB)) void attend_many_kernel(const AttendPlan p) {
+  using elem = typename Tag::elem;
+  constexpr bool kF32 = Tag::dtype == CAFEQ_F32;
+  constexpr int kParts = kF32 ? 2 : 1, KT = many_keys(DB), NT = KT / 32, KS = 4 * DB, MT = 2 * DB, U = KT / 16;
+  constexpr int kTile = 32 * QT * kWaves, E = (KT * KS + kThreads - 1) / kThreads;
+  constexpr int kRunK = KT + 1, kRunV = 64 * DB + 1, kBufK = 2 * KS * kRunK, kBuf = kBufK + 2 * U * kRunV;
+  extern __shared__ __align__(16) half8_t buf[];
+  const cafeq_cache& c = p.c;
+  const cafeq_attention& a = p.a;
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int head = blockIdx.x % c.heads, split = blockIdx.y, shift_b = p.shift, B = c.block, d = EXACT ? 64 * DB : c.d, chunks = d / 16;
+  // later rows of a sequence reach more keys: first
+  const int64_t w = (gridDim.x - 1 - blockIdx.x) / c.heads;
+  const int i = sequence_of(p.units, a.starts, c.sequences, int(a.n), w);
+  if (i < 0) return;
+  const int first = int(w - p.units.base(min(max(a.starts[i], 0), int(a.n)), i)) * kTile;
+  const Reach r = reach_of(c, a, i, p.rep, first, kTile);
+  if (first >= r.rows || r.rows <= p.few_rows) return;
+  const int c0 = r.lo / KT, c1 = max(c0, (r.hi + KT - 1) / KT), used = max(1, (c1 - c0 + p.span - 1) / p.span);
+  if (split >= used) return;
+  const int begin = c0 + split * p.span, end = min(c1, begin + p.span);
+
+  // rows of the wave
+  const int wfirst = first + wave * 32 * QT, wlast = min(wfirst + 32 * QT, r.rows) - 1;
+  const int wlo = key_begin(a, r.pos0 + wfirst / p.rep), whi = wlast < wfirst ? 0 : key_end(a, r.len, r.pos0 + wlast / p.rep);
+  const int all_lo = key_begin(a, r.pos0 + max(wlast, 0) / p.rep), all_hi = key_end(a, r.len, r.pos0 + wfirst / p.rep);
+  int klo[QT], khi[QT];
+  half8_t q[kParts][QT][KS];
+  float unit[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int R = wfirst + 32 * t + l32, token = R / p.rep;
+    const bool live = R < r.rows;
+    const int pos = r.pos0 + token;
+    klo[t] = live ? key_begin(a, pos) : 0;
+    khi[t] = live ? key_end(a, r.len, pos) : 0;
+    const elem* x = static_cast<const elem*>(a.q) + int64_t(r.row0 + (live ? token : 0)) * a.ldq + int64_t(head * p.rep + (live ? R - token * p.rep : 0)) * a.hsq;
+    float v[KS][8];
+    uint32_t bits = 0;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const bool in = live && (EXACT || 16 * s < d);
+      const elem* y = x + (EXACT || 16 * s < d ? 16 * s + 8 * h : 0);
+#pragma unroll
+      for (int e = 0; e < 8; e += 4) {
+        const float4 f = load4(y + e);
+        v[s][e] = in ? f.x : 0.f; v[s][e + 1] = in ? f.y : 0.f; v[s][e + 2] = in ? f.z : 0.f; v[s][e + 3] = in ? f.w : 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) bits = max(bits, __float_as_uint(v[s][e]) & 0x7FFFFFFFu);
+    }
+    bits = max(bits, uint32_t(__shfl_xor(int(bits), 32)));
+    const QueryScale qs = query_scale(bits, a);
+    unit[t] = qs.unit;
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const float f0 = v[s][e] * qs.up, f1 = v[s][e + 1] * qs.up;
+        const half2_t x2 = to_half(f0, f1);
+        q[0][t][s][e] = x2[0];
+        q[0][t][s][e + 1] = x2[1];
+        if constexpr (kF32) {
+          const half2_t y2 = to_half(f0 - float(x2[0]), f1 - float(x2[1]));
+          q[1][t][s][e] = y2[0];
+          q[1][t][s][e + 1] = y2[1];
+        }
+      }
+  }
+
+  // what this thread brings of every tile: 16 channels of a key, 16 keys of a channel
+  const int32_t* table = c.table + int64_t(i) * c.width;
+  int kkey[E], kat[E], klds[E], vrun[E], vat[E], vlds[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int n = tid + e * kThreads, key = min(n / chunks, KT - 1), s = n % chunks;
+    kkey[e] = key;
+    kat[e] = key * d + 16 * s;
+    klds[e] = n < KT * chunks ? 2 * s * kRunK + key : -1;
+    const int u = n % U, ch = min(n / U, d - 1);
+    vrun[e] = 16 * u;
+    vat[e] = ch * B;
+    vlds[e] = n < U * d ? kBufK + 2 * u * kRunV + ch : -1;
+  }
+  auto page_at = [&](int key) {
+    const int entry = table[min(key >> shift_b, c.width - 1)];
+    return key < r.len && entry >= 0 && entry < c.pages ? entry : -1;
+  };
+  int kpage[E], vpage[E], spage;     // pages of the tile that is requested next; lanes 0 .. U - 1 hold those of its runs of 16 keys
+  auto pages_of = [&](int tile) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      kpage[e] = page_at(tile * KT + kkey[e]);
+      vpage[e] = page_at(tile * KT + vrun[e]);
+    }
+    spage = page_at(tile * KT + 16 * (lane & (U - 1)));
+  };
+  uint4 kc[E], vc[E];
+  float ks, vs;
+  bool hole;
+  auto request = [&](int tile) {
+    const int in_page = B - 1;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      // key * d + channel within the page: the tile's first key may lie inside a page, and a page inside the tile
+      const int8_t* k = c.k + (int64_t(max(kpage[e], 0)) * c.heads + head) * B * d;
+      const int key = (tile * KT + kkey[e]) & in_page;
+      kc[e] = *reinterpret_cast<const uint4*>(k + key * d + (kat[e] - kkey[e] * d));
+      const int8_t* v = c.v + (int64_t(max(vpage[e], 0)) * c.heads + head) * B * d;
+      vc[e] = *reinterpret_cast<const uint4*>(v + vat[e] + ((tile * KT + vrun[e]) & in_page));
+    }
+    const int64_t s = int64_t(max(spage, 0)) * c.heads + head;
+    ks = c.kscale[s];
+    vs = c.vscale[s];
+    hole = spage < 0;
+  };
+  auto put = [&](half8_t* to) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if (klds[e] >= 0) {
+        to[klds[e]] = half_codes(kc[e].x, kc[e].y);
+        to[klds[e] + kRunK] = half_codes(kc[e].z, kc[e].w);
+      }
+      if (vlds[e] >= 0) {
+        to[vlds[e]] = half_codes(vc[e].x, vc[e].z);
+        to[vlds[e] + kRunV] = half_codes(vc[e].y, vc[e].w);
+      }
+    }
+  };
+
+  f32x16_t o[QT][MT];
+  float M[QT], l[QT], mz[QT], lz[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    M[t] = mz[t] = kNoKey;
+    l[t] = lz[t] = 0.f;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) o[t][m] = f32x16_t{};
+  }
+
+  if (begin < end) {
+    pages_of(begin);
+    request(begin);
+    pages_of(begin + 1);
+    put(buf);
+  }
+  __syncthreads();
+  for (int tile = begin; tile < end; ++tile) {
+    const half8_t* now_buf = buf + ((tile - begin) & 1) * kBuf;
+    const float tks = ks, tvs = vs;
+    const bool thole = hole;
+    if (tile + 1 < end) {
+      request(tile + 1);
+      pages_of(tile + 2);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int key0 = tile * KT + 32 * n;
+      if (key0 >= whi || key0 + 32 <= wlo) continue;
+      f32x16_t x[QT];
+#pragma unroll
+      for (int t = 0; t < QT; ++t) x[t] = f32x16_t{};
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        if (!EXACT && 16 * s >= d) continue;
+        const half8_t k = now_buf[(2 * s + h) * kRunK + 32 * n + l32];
+#pragma unroll
+        for (int e = kParts - 1; e >= 0; --e)
+#pragma unroll
+          for (int t = 0; t < QT; ++t) x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[e][t][s], x[t], 0, 0, 0);
+      }
+      // the two runs of 16 keys: results 0 .. 7 and 8 .. 15
+      ValueScale sc[2];
+      float ksc[2];
+      bool gone[2], odd = key0 < all_lo || key0 + 32 > all_hi;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        ksc[k] = lane_value(tks, 2 * n + k);
+        sc[k] = value_scale(lane_value(tvs, 2 * n + k));
+        gone[k] = __builtin_amdgcn_readlane(int(thole), 2 * n + k);
+        odd |= gone[k] || sc[k].zero || !(ksc[k] >= 0.f);
+      }
+      half8_t wt[kParts][QT][2];
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        float f[2] = {unit[t] * ksc[0], unit[t] * ksc[1]};
+        if (a.softcap > 0.f) {
+          const float in = 1.f / a.softcap, out = a.softcap * kLog2e;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[t][e] = capped<kF32>(x[t][e] * (f[e >> 3] * in), out);
+          f[0] = f[1] = 1.f;
+        }
+        float top = kNoKey;
+        const int from = klo[t] - key0 - 4 * h, to = khi[t] - key0 - 4 * h;
+        auto in = [&](int e) { return bool(int(8 * (e >> 2) + (e & 3) >= from) & int(8 * (e >> 2) + (e & 3) < to) & int(!gone[e >> 3])); };
+        if (!odd) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            float y = x[t][8 * k];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) y = fmaxf(y, x[t][8 * k + e]);
+            top = fmaxf(top, y * f[k] + sc[k].exp);
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            float y = kNoKey;
+#pragma unroll
+            for (int e = 8 * k; e < 8 * k + 8; ++e) y = in(e) ? fmaxf(y, x[t][e] * f[k]) : y;
+            if (sc[k].zero) {
+              // keys of a page of zeros count in the sum of weights only, on a maximum of their own
+              const float most = fmaxf(mz[t], other_half(y));
+              lz[t] *= __builtin_amdgcn_exp2f(mz[t] - most);
+              mz[t] = most;
+#pragma unroll
+              for (int e = 8 * k; e < 8 * k + 8; ++e) lz[t] += in(e) ? __builtin_amdgcn_exp2f(x[t][e] * f[k] - most) : 0.f;
+            } else {
+              top = y == kNoKey ? top : fmaxf(top, y + sc[k].exp);
+            }
+          }
+        }
+        const float most = fmaxf(M[t], ceilf(other_half(top)) - kTop);
+        if (__ballot(most != M[t])) {
+          const float back = __builtin_amdgcn_exp2f(M[t] - most);
+          l[t] *= back;
+#pragma unroll
+          for (int m = 0; m < MT; ++m) o[t][m] *= back;
+          M[t] = most;
+        }
+        float P[16];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const float shift = sc[k].exp - M[t];
+          float sum = 0.f;
+#pragma unroll
+          for (int e = 8 * k; e < 8 * k + 8; ++e) P[e] = __builtin_amdgcn_exp2f(fmaf(x[t][e], f[k], shift));
+          if (odd) {
+#pragma unroll
+            for (int e = 8 * k; e < 8 * k + 8; ++e) P[e] = int(in(e)) & int(!sc[k].zero) ? P[e] : 0.f;
+          }
+#pragma unroll
+          for (int e = 8 * k; e < 8 * k + 8; ++e) {
+            sum += P[e];
+            P[e] *= sc[k].mant;
+          }
+          if (odd) {      // a scale that is no number must not reach keys that do not count
+#pragma unroll
+            for (int e = 8 * k; e < 8 * k + 8; ++e) P[e] = int(in(e)) & int(!sc[k].zero) ? P[e] : 0.f;
+          }
+          l[t] = fmaf(sum, sc[k].inv, l[t]);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          const half2_t y = to_half(P[e], P[e + 1]);
+          wt[0][t][e >> 3][e & 7] = y[0];
+          wt[0][t][e >> 3][(e & 7) + 1] = y[1];
+          if constexpr (kF32) {
+            const half2_t rest = to_half(P[e] - float(y[0]), P[e + 1] - float(y[1]));
+            wt[1][t][e >> 3][e & 7] = rest[0];
+            wt[1][t][e >> 3][(e & 7) + 1] = rest[1];
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          if (!EXACT && 32 * m >= d) continue;
+          const half8_t v = now_buf[kBufK + (2 * (2 * n + u) + h) * kRunV + 32 * m + l32];
+#pragma unroll
+          for (int e = kParts - 1; e >= 0; --e)
+#pragma unroll
+            for (int t = 0; t < QT; ++t) o[t][m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, wt[e][t][u], o[t][m], 0, 0, 0);
+        }
+    }
+    if (tile + 1 < end) put(buf + ((tile + 1 - begin) & 1) * kBuf);
+    __syncthreads();
+  }
+
+  const int64_t part = ((w * c.heads + head) * p.splits + split) * kTile;
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int row = wave * 32 * QT + 32 * t + l32, R = first + row;
+    float sum = l[t] + __shfl_xor(l[t], 32), sumz = lz[t] + __shfl_xor(lz[t], 32);
+    const float both = fmaxf(M[t], mz[t]), own = __builtin_amdgcn_exp2f(M[t] - both);
+    const float total = sum * own + sumz * __builtin_amdgcn_exp2f(mz[t] - both);
+    if (R >= r.rows) continue;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int ch = 32 * m + 2 * e + 4 * h;
+        if (!EXACT && ch >= d) continue;
+        const f32x4_t v = f32x4_t{o[t][m][e], o[t][m][e + 1], o[t][m][e + 2], o[t][m][e + 3]} * own;
+        if (used > 1) *reinterpret_cast<f32x4_t*>(p.parts + (part + row) * d + ch) = v;
+        else store_row<Tag>(p, r, R, head, ch, v, both, total);
+      }
+    if (used > 1 && h == 0) *reinterpret_cast<float2*>(p.sums + 2 * (part + row)) = make_float2(both, total);
+  }
+}
+
+// The parts of a tile's rows joined in their order, four channels a thread.
+template <class Tag, int DB, int QT>
+__global__ __launch_bounds__(kThreads) void attend_many_join_kernel(const AttendPlan p) {
+  constexpr int kTile = 32 * QT * kWaves, KT = many_keys(DB);
+  const cafeq_cache& c = p.c;
+  const int head = blockIdx.x % c.heads, d = c.d, per = d / 4;
+  const int64_t w = blockIdx.x / c.heads;
+  const int i = sequence_of(p.units, p.a.starts, c.sequences, int(p.a.n), w);
+  if (i < 0) return;
+  const int first = int(w - p.units.base(min(max(p.a.starts[i], 0), int(p.a.n)), i)) * kTile;
+  const Reach r = reach_of(c, p.a, i, p.rep, first, kTile);
+  if (first >= r.rows || r.rows <= p.few_rows) return;
+  const int c0 = r.lo / KT, c1 = max(c0, (r.hi + KT - 1) / KT), used = (c1 - c0 + p.span - 1) / p.span;
+  const int e = blockIdx.y * kThreads + threadIdx.x, row = e / per, ch = e % per * 4;
+  if (used <= 1 || row >= kTile || first + row >= r.rows) return;
+  const int64_t part = (w * c.heads + head) * p.splits * kTile + row;
+  float big = kNoKey, total = 0.f;
+  for (int s = 0; s < used; ++s) big = fmaxf(big, p.sums[2 * (part + int64_t(s) * kTile)]);
+  f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = 0; s < used; ++s) {
+    const int64_t at = part + int64_t(s) * kTile;
+    const float2 m = *reinterpret_cast<const float2*>(p.sums + 2 * at);
+    const float f = __builtin_amdgcn_exp2f(m.x - big);
+    total += m.y * f;
+    v += *reinterpret_cast<const f32x4_t*>(p.parts + at * d + ch) * f;
+  }
+  store_row<Tag>(p, r, first + row, head, ch, v, big, total);
+}
+
+template <class Tag, int DB, bool EXACT>
+int launch(const AttendPlan& p, hipStream_t st) {
+  constexpr int QT = many_tiles(Tag::dtype, DB), KT = many_keys(DB), kTile = 32 * QT * kWaves;
+  constexpr size_t lds = 2 * 16 * (2 * 4 * DB * (KT + 1) + 2 * (KT / 16) * (64 * DB + 1));
+  const auto kern = attend_many_kernel<Tag, DB, EXACT, QT>;
+  if (lds > 65536) {
+    static const bool ok = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds)) == hipSuccess;
+    if (!ok) return CAFEQ_ERR_LAUNCH;
+  }
+  // the heads innermost: workgroups go round the eight XCDs in turn, so that a head's tiles stay behind one L2
+  const unsigned units = unsigned(p.units.count(p.a.n, p.c.sequences) * p.c.heads);
+  hipLaunchKernelGGL(kern, dim3(units, unsigned(p.splits)), dim3(kThreads), lds, st, p);
+  CAFEQ_CHECK_LAUNCH();
+  if (p.splits > 1) {
+    const unsigned y = unsigned((kTile * (p.c.d / 4) + kThreads - 1) / kThreads);
+    hipLaunchKernelGGL((attend_many_join_kernel<Tag, DB, QT>), dim3(units, y), dim3(kThreads), 0, st, p);
+    CAFEQ_CHECK_LAUNCH();
+  }
+  return CAFEQ_OK;
+}
+
+template <class Tag>
+int launch_type(const AttendPlan& p, hipStream_t st) {
+  switch (p.c.d) {
+    case 64: return launch<Tag, 1, true>(p, st);
+    case 128: return launch<Tag, 2, true>(p, st);
+    case 256: return launch<Tag, 4, true>(p, st);
+  }
+  switch ((p.c.d + 63) / 64) {
+    case 1: return launch<Tag, 1, false>(p, st);
+    case 2: return launch<Tag, 2, false>(p, st);
+    case 3: return launch<Tag, 3, false>(p, st);
+    default: return launch<Tag, 4, false>(p, st);
+  }
+}
+
+}  // namespace
+
+int launch_attend_many(const AttendPlan& p, hipStream_t st) {
+  return p.a.dtype == CAFEQ_F32 ? launch_type<F32Tag>(p, st) : launch_type<BF16Tag>(p, st);
+}
+
+}  // namespace cafeq

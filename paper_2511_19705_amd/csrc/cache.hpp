@@ -56,7 +56,8 @@ __device__ __forceinline__ int sequence_of(const Units& u, const int32_t* starts
     first += (seen - 1) * step;
     left = step > 1 ? min(step, sequences - first) : 0;
   }
-  return first;
+  // (starts out of order may have led elsewhere)
+  return sequences > 0 && u.base(min(max(starts[first], 0), n), first) <= w ? first : -1;
 }
 
 }  // namespace cafeq
