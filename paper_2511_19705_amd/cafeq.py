@@ -761,7 +761,8 @@ def _part(x, out, gain, d, dev, what):
             raise CafeqError("%s is not given" % what)
         return None, None
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        n, h = x.shape[:2]
+        out = torch.empty_strided((n, h, d), (h * d, d, 1), dtype=x.dtype, device=x.device)
     elif out.shape != x.shape or out.dtype is not x.dtype:
         raise CafeqError("out_%s must have the shape and type of %s" % (what, what))
     ldx, hsx = _head_rows(x, dev, what)
@@ -797,16 +798,21 @@ def rotate_heads(q, k, positions, freq, interleaved=False, norm=False, gain_q=No
     return out_q, out_k
 
 
-class KVCache(NamedTuple):
+class KVCache:
     """A cache as cafeq.h describes it: codes and scales of keys and values, the page of each block of a sequence, tokens of a sequence, rows that
-    hold a page."""
-    k: torch.Tensor
-    v: torch.Tensor
-    kscale: torch.Tensor
-    vscale: torch.Tensor
-    table: torch.Tensor
-    lengths: torch.Tensor
-    refs: torch.Tensor
+    hold a page.  Its tensors are checked at the first call and after one of them was replaced; their contents may change at will."""
+    __slots__ = ("k", "v", "kscale", "vscale", "table", "lengths", "refs", "_desc")
+    _fields = __slots__[:7]
+
+    def __init__(self, k, v, kscale, vscale, table, lengths, refs):
+        self.k, self.v, self.kscale, self.vscale, self.table, self.lengths, self.refs = k, v, kscale, vscale, table, lengths, refs
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_desc", None)
+
+    def _replace(self, **tensors):
+        return KVCache(**{**{n: getattr(self, n) for n in self._fields}, **tensors})
 
 
 def kv_cache(sequences, pages, heads, d, block=64, width=None, device=None):
@@ -824,16 +830,22 @@ def kv_cache(sequences, pages, heads, d, block=64, width=None, device=None):
 
 
 def _cache(c, dev):
-    """Descriptor of a KVCache on device number `dev`."""
+    """(descriptor, its reference for a call) of a KVCache on device number `dev`.  What the seven checks cost (8 us) is paid once."""
+    have = c._desc
+    if have is not None and have[2] == dev:
+        return have
     if len(c.k.shape) != 4 or len(c.table.shape) != 2:
         raise CafeqError("cache: k must be [pages][heads][block][d], table [sequences][width]")
     pages, heads, block, d = c.k.shape
     rows, width = c.table.shape
     i8, i32, f32 = torch.int8, torch.int32, torch.float32
-    return Cache(_operand(c.k, dev, i8, (pages, heads, block, d), "cache.k"), _operand(c.v, dev, i8, (pages, heads, d, block), "cache.v"),
+    desc = Cache(_operand(c.k, dev, i8, (pages, heads, block, d), "cache.k"), _operand(c.v, dev, i8, (pages, heads, d, block), "cache.v"),
                  _operand(c.kscale, dev, f32, (pages, heads), "cache.kscale"), _operand(c.vscale, dev, f32, (pages, heads), "cache.vscale"),
                  _operand(c.table, dev, i32, (rows, width), "cache.table"), _operand(c.lengths, dev, i32, (rows,), "cache.lengths"),
                  _operand(c.refs, dev, i32, (pages,), "cache.refs"), pages, rows, width, heads, d, block)
+    have = (desc, ctypes.byref(desc), dev, int(lib.cafeq_cache_pages_workspace_bytes(ctypes.byref(desc))))
+    object.__setattr__(c, "_desc", have)
+    return have
 
 
 def _starts(t, rows, dev, what="starts"):
@@ -846,14 +858,14 @@ def cache_append(cache, k, v, starts, longest=None):
     dev, kind = torch._C._cuda_getDevice(), _FLOATS.get(k.dtype)
     if kind is None or v.dtype is not k.dtype:
         raise CafeqError("k and v must be float32 or bfloat16, both the same")
-    c = _cache(cache, dev)
+    c, ref = _cache(cache, dev)[:2]
     n = k.shape[0]
     if k.shape != (n, c.heads, c.d) or v.shape != k.shape:
         raise CafeqError("k and v must be [n][%d][%d]" % (c.heads, c.d))
     (ldk, hsk), (ldv, hsv) = _head_rows(k, dev, "k"), _head_rows(v, dev, "v")
     ps = _starts(starts, c.sequences, dev)
     if n:
-        rc = lib.cafeq_cache_append(ctypes.byref(c), k.data_ptr(), v.data_ptr(), kind, n, ldk, hsk, ldv, hsv, ps, n if longest is None else longest,
+        rc = lib.cafeq_cache_append(ref, k.data_ptr(), v.data_ptr(), kind, n, ldk, hsk, ldv, hsv, ps, n if longest is None else longest,
                                     torch._C._cuda_getCurrentRawStream(dev))
         if rc:
             _check(rc)
@@ -864,11 +876,11 @@ def cache_values(cache, begin, starts, n, dtype=torch.float32):
     dev, kind = torch._C._cuda_getDevice(), _FLOATS.get(dtype)
     if kind is None:
         raise CafeqError("dtype must be float32 or bfloat16")
-    c = _cache(cache, dev)
+    c, ref = _cache(cache, dev)[:2]
     pb, ps = _operand(begin, dev, torch.int32, (c.sequences,), "begin"), _starts(starts, c.sequences, dev)
-    k, v = (torch.empty((n, c.heads, c.d), dtype=dtype, device=cache.k.device) for _ in range(2))
+    k, v = (cache.k.new_empty((n, c.heads, c.d), dtype=dtype) for _ in range(2))
     if n:
-        rc = lib.cafeq_cache_values(ctypes.byref(c), pb, ps, n, k.data_ptr(), v.data_ptr(), kind, torch._C._cuda_getCurrentRawStream(dev))
+        rc = lib.cafeq_cache_values(ref, pb, ps, n, k.data_ptr(), v.data_ptr(), kind, torch._C._cuda_getCurrentRawStream(dev))
         if rc:
             _check(rc)
     return k, v
@@ -880,13 +892,13 @@ def cache_attend(cache, q, starts, longest=None, scale=None, softcap=0.0, window
     dev, kind = torch._C._cuda_getDevice(), _FLOATS.get(q.dtype)
     if kind is None:
         raise CafeqError("q must be float32 or bfloat16")
-    c = _cache(cache, dev)
+    c, ref = _cache(cache, dev)[:2]
     if q.dim() != 3 or q.shape[2] != c.d or q.shape[1] < 1 or q.shape[1] % c.heads:
         raise CafeqError("q must be [n][a multiple of %d][%d]" % (c.heads, c.d))
     n, hq, d = q.shape
     ldq, hsq = _head_rows(q, dev, "q")
     if out is None:
-        out = torch.empty((n, hq, d), dtype=q.dtype, device=q.device)
+        out = torch.empty_strided((n, hq, d), (hq * d, d, 1), dtype=q.dtype, device=q.device)
         ldo, hso = hq * d, d
     else:
         if out.shape != q.shape or out.dtype is not q.dtype:
@@ -897,11 +909,11 @@ def cache_attend(cache, q, starts, longest=None, scale=None, softcap=0.0, window
                   _starts(starts, c.sequences, dev), kind, hq, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, softcap)
     if n:
         stream = torch._C._cuda_getCurrentRawStream(dev)
-        rc = lib.cafeq_cache_attend(ctypes.byref(c), ctypes.byref(a), None, stream)
-        if rc == _ERR_WORKSPACE:
-            # the buffer is of this call alone, so that streams share nothing
-            ws = q.new_empty(lib.cafeq_cache_attend_workspace_bytes(ctypes.byref(c), ctypes.byref(a)), dtype=torch.uint8)
-            rc = lib.cafeq_cache_attend(ctypes.byref(c), ctypes.byref(a), ws.data_ptr(), stream)
+        pa = ctypes.byref(a)
+        nbytes = lib.cafeq_cache_attend_workspace_bytes(ref, pa)
+        # the buffer is of this call alone, so that streams share nothing
+        ws = q.new_empty(nbytes, dtype=torch.uint8).data_ptr() if nbytes else None
+        rc = lib.cafeq_cache_attend(ref, pa, ws, stream)
         if rc:
             _check(rc)
     return (out, sums) if lse else out
@@ -915,31 +927,28 @@ class Reserved(NamedTuple):
 
 def _pages_call(cache):
     dev = torch._C._cuda_getDevice()
-    c = _cache(cache, dev)
-    ws = torch.empty(max(256, lib.cafeq_cache_pages_workspace_bytes(ctypes.byref(c))), dtype=torch.uint8, device=cache.k.device)
-    return dev, c, ws, torch._C._cuda_getCurrentRawStream(dev)
+    c, ref, _, nbytes = _cache(cache, dev)
+    return dev, c, ref, cache.k.new_empty(max(256, nbytes), dtype=torch.uint8), torch._C._cuda_getCurrentRawStream(dev)
 
 
 def cache_reserve(cache, starts, n):
     """cafeq_cache_reserve: room for starts[i + 1] - starts[i] more tokens of each sequence, n in all.  Nothing waits: a caller that cannot be
     sure of room reads `missing` (one int32 on the device); where it is not 0 nothing has changed and positions hold nothing."""
-    dev, c, ws, stream = _pages_call(cache)
-    positions = torch.empty(n, dtype=torch.int32, device=cache.k.device)
-    missing = torch.empty(1, dtype=torch.int32, device=cache.k.device)
-    _check(lib.cafeq_cache_reserve(ctypes.byref(c), _starts(starts, c.sequences, dev), n, positions.data_ptr() if n else None, missing.data_ptr(), ws.data_ptr(),
-                                   stream))
+    dev, c, ref, ws, stream = _pages_call(cache)
+    positions, missing = cache.refs.new_empty(n), cache.refs.new_empty(1)
+    _check(lib.cafeq_cache_reserve(ref, _starts(starts, c.sequences, dev), n, positions.data_ptr() if n else None, missing.data_ptr(), ws.data_ptr(), stream))
     return Reserved(positions, missing)
 
 
 def cache_reorder(cache, sources):
     """cafeq_cache_reorder: row i takes over what row sources[i] held (int32 [sequences]; outside the rows: nothing, which lets its pages go)."""
-    dev, c, ws, stream = _pages_call(cache)
-    _check(lib.cafeq_cache_reorder(ctypes.byref(c), _operand(sources, dev, torch.int32, (c.sequences,), "sources"), ws.data_ptr(), stream))
+    dev, c, ref, ws, stream = _pages_call(cache)
+    _check(lib.cafeq_cache_reorder(ref, _operand(sources, dev, torch.int32, (c.sequences,), "sources"), ws.data_ptr(), stream))
 
 
 def cache_compact(cache):
     """cafeq_cache_compact: pages in use move to the front of the pool.  Returns how many there are (int32 [1] on the device)."""
-    dev, c, ws, stream = _pages_call(cache)
-    used = torch.empty(1, dtype=torch.int32, device=cache.k.device)
-    _check(lib.cafeq_cache_compact(ctypes.byref(c), used.data_ptr(), ws.data_ptr(), stream))
+    dev, c, ref, ws, stream = _pages_call(cache)
+    used = cache.refs.new_empty(1)
+    _check(lib.cafeq_cache_compact(ref, used.data_ptr(), ws.data_ptr(), stream))
     return used

@@ -5,7 +5,7 @@
 namespace cafeq {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kFewThreads = 64;
 
 struct AppendArgs {
   cafeq_cache c;
@@ -44,15 +44,20 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t w, float ratio, int keep) 
   return r;
 }
 
-// A workgroup stores what a sequence's new tokens bring to one page and head, keys or values.
-template <class Tag>
-__global__ __launch_bounds__(kThreads) void append_kernel(const AppendArgs a) {
+__device__ __forceinline__ uint4 rescaled(const uint4& w, float ratio, int keep) {
+  return make_uint4(rescaled(w.x, ratio, keep), rescaled(w.y, ratio, keep - 4), rescaled(w.z, ratio, keep - 8), rescaled(w.w, ratio, keep - 12));
+}
+
+// A workgroup stores what a sequence's new tokens bring to one page and head, keys or values.  A thread takes eight channels of four tokens that
+// share a dword of v, reads them once, and writes them as eight codes a token (k) or four a channel (v).  NG: such groups a thread holds.
+template <class Tag, int T, int NG>
+__global__ __launch_bounds__(T) void append_kernel(const AppendArgs a) {
   using elem = typename Tag::elem;
-  __shared__ uint32_t top[kThreads / 64];
+  __shared__ uint32_t top[T / 64];
   const cafeq_cache& c = a.c;
   const int head = blockIdx.y, side = blockIdx.z, tid = threadIdx.x, B = c.block, d = c.d;
   const int64_t w = blockIdx.x;
-  const int i = sequence_of(a.units, a.starts, c.sequences, a.n, w);
+  const int i = a.longest == 1 ? int(w) : sequence_of(a.units, a.starts, c.sequences, a.n, w);
   if (i < 0) return;
   const RowRange r = rows_of(a.starts, i, a.n);
   const int len = tokens_of(c, i), pos0 = len - (r.hi - r.lo);                 // row lo + j stands at pos0 + j
@@ -63,55 +68,75 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const AppendArgs a) {
   const int page = page_of(c, i, int(block));
   if (page < 0) return;
   const int f = int(first - block * B), m = int(last - first), per = d / 8;
-  const elem* x = static_cast<const elem*>(a.x[side]) + (r.lo + first - pos0) * a.ld[side] + head * a.hs[side];
+  const int64_t ld = a.ld[side];
+  // row of slot 0 of the page
+  const elem* x = static_cast<const elem*>(a.x[side]) + (r.lo + block * B - pos0) * ld + head * a.hs[side];
   const int64_t at = int64_t(page) * c.heads + head;
   int8_t* codes = (side ? c.v : c.k) + at * B * d;
   float* scale = (side ? c.vscale : c.kscale) + at;
 
+  const int group0 = f >> 2, groups = ((f + m - 1) >> 2) - group0 + 1, total = groups * per;
+  float v[NG][4][8];
   uint32_t big = 0;
-  for (int e = tid; e < m * per; e += kThreads) {
-    float v[8];
-    get8(x + (e / per) * a.ld[side] + e % per * 8, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) big = max(big, mag(v[j]));
+  for (int n = 0; n < NG; ++n) {
+    const int e = tid + n * T, ch = (side ? e / groups : e % per) * 8, slot = 4 * (group0 + (side ? e % groups : e / per));
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      if (e < total && slot + s >= f && slot + s < f + m) {
+        get8(x + (slot + s) * ld + ch, v[n][s]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) big = max(big, mag(v[n][s][j]));
+      }
   }
-  for (int s = 1; s < 64; s <<= 1) big = max(big, uint32_t(__shfl_xor(int(big), s)));
-  if ((tid & 63) == 0) top[tid >> 6] = big;
   const float old = f > 0 ? __uint_as_float(mag(*scale)) : 0.f;
-  __syncthreads();
-  for (int j = 0; j < kThreads / 64; ++j) big = max(big, top[j]);
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) big = max(big, uint32_t(__shfl_xor(int(big), s)));
+  if constexpr (T > 64) {
+    if ((tid & 63) == 0) top[tid >> 6] = big;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < T / 64; ++j) big = max(big, top[j]);
+  }
   // compared as bits: a NaN lies above an infinity, and that above all numbers
   const float s = __uint_as_float(max(mag(old), mag(__fdiv_rn(__uint_as_float(big), 127.f))));
   const bool number = mag(s) < 0x7F800000u;
   const float inv = number && s > 0.f ? fminf(__fdiv_rn(1.f, s), FLT_MAX) : 0.f;
   if (f > 0 && mag(s) != mag(old)) {
     const float ratio = number ? __fdiv_rn(old, s) : 0.f;
-    if (side == 0) {
-      for (int e = tid; e < f * d / 4; e += kThreads) {
-        uint32_t* p = reinterpret_cast<uint32_t*>(codes) + e;
-        *p = rescaled(*p, ratio, 4);
-      }
-    } else {
-      const int words = (f + 3) / 4;
-      for (int e = tid; e < d * words; e += kThreads) {
-        uint32_t* p = reinterpret_cast<uint32_t*>(codes + e / words * B) + e % words;
-        *p = rescaled(*p, ratio, min(4, f - 4 * (e % words)));
-      }
+    const int runs = side ? (f + 15) / 16 : d / 16, count = side ? d * runs : f * runs;
+    for (int e = tid; e < count; e += T) {
+      uint4* p = reinterpret_cast<uint4*>(codes + (side ? e / runs * B : e / runs * d)) + e % runs;
+      *p = rescaled(*p, ratio, side ? f - 16 * (e % runs) : 16);
     }
+    __syncthreads();      // a word of v may hold earlier and new tokens
   }
   if (tid == 0) *scale = s;
-  __syncthreads();      // a word of v may hold earlier and new tokens
-  for (int e = tid; e < m * per; e += kThreads) {
-    const int t = e / per, ch = e % per * 8;
-    float v[8];
-    get8(x + t * a.ld[side] + ch, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = number ? code_of(v[j], inv) : 0.f;
+  for (int n = 0; n < NG; ++n) {
+    const int e = tid + n * T, ch = (side ? e / groups : e % per) * 8, slot = 4 * (group0 + (side ? e % groups : e / per));
+    if (e >= total) continue;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[n][q][j] = number ? code_of(v[n][q][j], inv) : 0.f;
+    const int lo = f - slot, hi = f + m - slot;      // of the four tokens
     if (side == 0) {
-      *reinterpret_cast<uint2*>(codes + (f + t) * d + ch) = make_uint2(pack4(v[0], v[1], v[2], v[3]), pack4(v[4], v[5], v[6], v[7]));
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (q >= lo && q < hi)
+          *reinterpret_cast<uint2*>(codes + (slot + q) * d + ch) =
+              make_uint2(pack4(v[n][q][0], v[n][q][1], v[n][q][2], v[n][q][3]), pack4(v[n][q][4], v[n][q][5], v[n][q][6], v[n][q][7]));
+    } else if (lo <= 0 && hi >= 4) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) *reinterpret_cast<uint32_t*>(codes + (ch + j) * B + slot) = pack4(v[n][0][j], v[n][1][j], v[n][2][j], v[n][3][j]);
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) codes[(ch + j) * B + f + t] = int8_t(int(v[j]));
+      for (int q = 0; q < 4; ++q)
+        if (q >= lo && q < hi) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) codes[(ch + j) * B + slot + q] = int8_t(int(v[n][q][j]));
+        }
     }
   }
 }
@@ -143,22 +168,59 @@ __global__ __launch_bounds__(kThreads) void values_kernel(const ValueArgs a) {
   const int64_t at = int64_t(max(page, 0)) * c.heads + head;
   const int8_t* codes = (side ? c.v : c.k) + at * B * d;
   const float s = page < 0 ? 0.f : (side ? c.vscale : c.kscale)[at];
-  elem* out = static_cast<elem*>(a.out[side]) + ((r.lo + first - pos0) * c.heads + head) * d;
+  // row of slot 0 of the page
+  elem* out = static_cast<elem*>(a.out[side]) + ((r.lo + block * B - pos0) * c.heads + head) * d;
   const int f = int(first - block * B), m = int(last - first), per = d / 8;
-  for (int e = tid; e < m * per; e += kThreads) {
-    const int t = side ? e % m : e / per, ch = side ? e / m * 8 : e % per * 8;
-    const bool there = page >= 0 && first + t < len;
-    float v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = there ? __fmul_rn(float(side ? codes[(ch + j) * B + f + t] : codes[(f + t) * d + ch + j]), s) : 0.f;
-    elem* o = out + int64_t(t) * c.heads * d + ch;
+  const int64_t ld = int64_t(c.heads) * d;
+  const int known = page < 0 ? 0 : int(min(int64_t(B), len - block * B));      // slots behind it, and of pages that are not there: zeros
+  auto store = [&](int slot, int ch, const float* v) {
+    elem* o = out + slot * ld + ch;
     if constexpr (Tag::dtype == CAFEQ_F32) {
       reinterpret_cast<float4*>(o)[0] = make_float4(v[0], v[1], v[2], v[3]);
       reinterpret_cast<float4*>(o)[1] = make_float4(v[4], v[5], v[6], v[7]);
     } else {
       *reinterpret_cast<uint4*>(o) = make_uint4(bf16_bits(v[0], v[1]), bf16_bits(v[2], v[3]), bf16_bits(v[4], v[5]), bf16_bits(v[6], v[7]));
     }
+  };
+  if (side == 0) {
+    for (int e = tid; e < m * per; e += kThreads) {
+      const int slot = f + e / per, ch = e % per * 8;
+      float v[8];
+      const uint2 q = slot < known ? *reinterpret_cast<const uint2*>(codes + slot * d + ch) : make_uint2(0u, 0u);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(float(int8_t((j < 4 ? q.x : q.y) >> (8 * (j & 3)))), slot < known ? s : 0.f);
+      store(slot, ch, v);
+    }
+    return;
   }
+  // eight channels of four tokens that share a dword
+  const int group0 = f >> 2, groups = ((f + m - 1) >> 2) - group0 + 1;
+  for (int e = tid; e < groups * per; e += kThreads) {
+    const int slot = 4 * (group0 + e % groups), ch = e / groups * 8;
+    uint32_t q[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[j] = page < 0 ? 0u : *reinterpret_cast<const uint32_t*>(codes + (ch + j) * B + slot);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (slot + k < f || slot + k >= f + m) continue;
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = slot + k < known ? __fmul_rn(float(int8_t(q[j] >> (8 * k))), s) : 0.f;
+      store(slot + k, ch, v);
+    }
+  }
+}
+
+template <class Tag>
+int launch_append(const AppendArgs& a, hipStream_t st) {
+  const dim3 grid(unsigned(a.units.count(a.n, a.c.sequences)), unsigned(a.c.heads), 2);
+  const int groups = a.c.block / 4 * (a.c.d / 8);      // at most so many in a page
+  if (a.longest == 1) hipLaunchKernelGGL((append_kernel<Tag, kFewThreads, 1>), grid, dim3(kFewThreads), 0, st, a);
+  else if (groups <= kThreads) hipLaunchKernelGGL((append_kernel<Tag, kThreads, 1>), grid, dim3(kThreads), 0, st, a);
+  else if (groups <= 2 * kThreads) hipLaunchKernelGGL((append_kernel<Tag, kThreads, 2>), grid, dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL((append_kernel<Tag, kThreads, 4>), grid, dim3(kThreads), 0, st, a);
+  CAFEQ_CHECK_LAUNCH();
+  return CAFEQ_OK;
 }
 
 }  // namespace
@@ -182,12 +244,8 @@ int cafeq_cache_append(const cafeq_cache* cache, const void* k, const void* v, i
   // a sequence's tokens touch at most floor of their number over the block, plus 2, pages; one token a sequence: one
   const Units u = longest == 1 ? Units{0, 1, 1} : Units{1, cache->block, 2};
   const AppendArgs a{*cache, {k, v}, {ldk, ldv}, {hsk, hsv}, starts, int(n), int(longest), u};
-  const dim3 grid(unsigned(u.count(n, cache->sequences)), unsigned(cache->heads), 2);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (dtype == CAFEQ_F32) hipLaunchKernelGGL((append_kernel<F32Tag>), grid, dim3(kThreads), 0, st, a);
-  else hipLaunchKernelGGL((append_kernel<BF16Tag>), grid, dim3(kThreads), 0, st, a);
-  CAFEQ_CHECK_LAUNCH();
-  return CAFEQ_OK;
+  return dtype == CAFEQ_F32 ? launch_append<F32Tag>(a, st) : launch_append<BF16Tag>(a, st);
 }
 
 int cafeq_cache_values(const cafeq_cache* cache, const int32_t* begin, const int32_t* starts, int64_t n, void* k, void* v, int dtype,

@@ -7,6 +7,7 @@ namespace cafeq {
 namespace {
 
 constexpr int kScan = 1024, kCopy = 256;
+constexpr int64_t kSmallTable = 16384;      // entries of a table that one workgroup reorders in 64 KB of LDS
 
 // Scratch of all three calls, int32 throughout
 struct PageWs {
@@ -173,6 +174,26 @@ __global__ __launch_bounds__(kCopy) void reorder_kernel(const cafeq_cache c, con
   if (threadIdx.x == 0) c.lengths[i] = len;
 }
 
+// The same for a table that LDS holds: one workgroup, one launch.
+__global__ __launch_bounds__(kScan) void reorder_small_kernel(const cafeq_cache c, const int32_t* sources) {
+  extern __shared__ int32_t held[];      // the table, then the lengths
+  const int tid = threadIdx.x, total = c.sequences * c.width, B = c.block;
+  int32_t* lengths = held + total;
+  for (int e = tid; e < total; e += kScan) held[e] = c.table[e];
+  for (int e = tid; e < c.sequences; e += kScan) lengths[e] = tokens_of(c, e);
+  __syncthreads();
+  for (int e = tid; e < total; e += kScan) {
+    const int i = e / c.width, b = e - i * c.width, from = sources[i];
+    if (from == i) continue;
+    const bool some = from >= 0 && from < c.sequences;
+    const int p = some && b < blocks_of(lengths[from], B) ? held[from * c.width + b] : -1, q = b < blocks_of(lengths[i], B) ? held[e] : -1;
+    c.table[e] = p;
+    if (p >= 0 && p < c.pages) atomicAdd(c.refs + p, 1);
+    if (q >= 0 && q < c.pages) atomicSub(c.refs + q, 1);
+    if (b == 0) c.lengths[i] = some ? lengths[from] : 0;
+  }
+}
+
 __global__ __launch_bounds__(kScan) void plan_compact_kernel(const cafeq_cache c, const PageWs w, int32_t* used) {
   const int tid = threadIdx.x;
   int count = 0, total;
@@ -269,6 +290,11 @@ int cafeq_cache_reorder(const cafeq_cache* cache, const int32_t* sources, void* 
   hipStream_t st = static_cast<hipStream_t>(stream);
   const PageWs w = page_ws(*cache, ws);
   const int64_t entries = int64_t(cache->sequences) * cache->width;
+  if (entries + cache->sequences <= kSmallTable) {
+    hipLaunchKernelGGL(reorder_small_kernel, dim3(1), dim3(kScan), size_t(entries + cache->sequences) * sizeof(int32_t), st, *cache, sources);
+    CAFEQ_CHECK_LAUNCH();
+    return CAFEQ_OK;
+  }
   hipLaunchKernelGGL(keep_table_kernel, dim3(unsigned(std::min<int64_t>(1024, (entries + kCopy - 1) / kCopy))), dim3(kCopy), 0, st, *cache, w);
   CAFEQ_CHECK_LAUNCH();
   hipLaunchKernelGGL(reorder_kernel, dim3(unsigned(cache->sequences)), dim3(kCopy), 0, st, *cache, w, sources);
