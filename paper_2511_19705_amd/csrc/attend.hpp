@@ -42,11 +42,11 @@ __device__ __forceinline__ half2_t to_half(float a, float b) {
   typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(half2_t, __builtin_convertvector((f32x2{a, b}), f16x2));
 }
-// out tanh(z); for results of bfloat16 by the hardware's exponential, good to 2^-22 of `out`
+// out tanh(z); for results of bfloat16, where z comes times 2 log2 e, by the hardware's exponential, good to 2^-22 of `out`
 template <bool F32>
 __device__ __forceinline__ float capped(float z, float out) {
   if constexpr (F32) return tanhf(z) * out;
-  else return out - 2.f * out * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.f * kLog2e * z));
+  else return fmaf(-2.f * out, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z)), out);
 }
 
 // The rows of one tile and what of the keys they reach.  Row R of a sequence and key head is token R / rep, query head R % rep of the group.

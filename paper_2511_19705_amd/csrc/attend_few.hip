@@ -203,7 +203,7 @@ __global__ __launch_bounds__(kThreads, Tag::dtype == CAFEQ_F32 && DB == 4 ? 1 : 
     }
     if (next < end) load_k(next);
     if (a.softcap > 0.f) {
-      const float in = 1.f / a.softcap, out = a.softcap * kLog2e;
+      const float in = kF32 ? 1.f / a.softcap : 2.f * kLog2e * __builtin_amdgcn_rcpf(a.softcap), out = a.softcap * kLog2e;
 #pragma unroll
       for (int n = 0; n < NS; ++n) {
 #pragma unroll

@@ -19,7 +19,8 @@ __device__ __forceinline__ float lane_value(float v, int lane) { return __uint_a
 // and of 32 keys those with key / 4 % 2 = l / 32: results i of a product are keys 8 (i / 4) + 4 (l / 32) + i % 4, weights 8 u .. 8 u + 7 what it gives to step u of
 // the second product.  LDS: K as [16 channels][half][key], V as [16 keys][half][channel] of eight float16 each, a place of 16 bytes
 // behind every run so that lanes that write side by side hit different banks.  Two buffers: the next tile's codes are on their way while this one is multiplied.
-template <class Tag, int DB, bool EXACT, int QT>
+// ONE: a tile's keys are of one page.
+template <class Tag, int DB, bool EXACT, bool ONE, int QT>
 __global__ __launch_bounds__(kThreads, many_waves(Tag::dtype, DB)) void attend_many_kernel(const AttendPlan p) {
   using elem = typename Tag::elem;
   constexpr bool kF32 = Tag::dtype == CAFEQ_F32;
@@ -111,31 +112,50 @@ __global__ __launch_bounds__(kThreads, many_waves(Tag::dtype, DB)) void attend_m
   };
   int kpage[E], vpage[E], spage;     // pages of the tile that is requested next; lanes 0 .. U - 1 hold those of its runs of 16 keys
   auto pages_of = [&](int tile) {
+    if constexpr (ONE) {
+      spage = page_at(tile * KT);
+    } else {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      kpage[e] = page_at(tile * KT + kkey[e]);
-      vpage[e] = page_at(tile * KT + vrun[e]);
+      for (int e = 0; e < E; ++e) {
+        kpage[e] = page_at(tile * KT + kkey[e]);
+        vpage[e] = page_at(tile * KT + vrun[e]);
+      }
+      spage = page_at(tile * KT + 16 * (lane & (U - 1)));
     }
-    spage = page_at(tile * KT + 16 * (lane & (U - 1)));
   };
   uint4 kc[E], vc[E];
   float ks, vs;
   bool hole;
   auto request = [&](int tile) {
     const int in_page = B - 1;
+    if constexpr (ONE) {
+      // one page: its place is the wave's, a thread's part of it stays
+      const int page = __builtin_amdgcn_readfirstlane(spage), key = (tile * KT) & in_page;
+      const int64_t at = int64_t(max(page, 0)) * c.heads + head;
+      const int8_t *k = c.k + (at * B + key) * d, *v = c.v + at * B * d + key;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      // key * d + channel within the page: the tile's first key may lie inside a page, and a page inside the tile
-      const int8_t* k = c.k + (int64_t(max(kpage[e], 0)) * c.heads + head) * B * d;
-      const int key = (tile * KT + kkey[e]) & in_page;
-      kc[e] = *reinterpret_cast<const uint4*>(k + key * d + (kat[e] - kkey[e] * d));
-      const int8_t* v = c.v + (int64_t(max(vpage[e], 0)) * c.heads + head) * B * d;
-      vc[e] = *reinterpret_cast<const uint4*>(v + vat[e] + ((tile * KT + vrun[e]) & in_page));
+      for (int e = 0; e < E; ++e) {
+        kc[e] = *reinterpret_cast<const uint4*>(k + uint32_t(kat[e]));
+        vc[e] = *reinterpret_cast<const uint4*>(v + uint32_t(vat[e] + vrun[e]));
+      }
+      ks = c.kscale[at];
+      vs = c.vscale[at];
+      hole = page < 0;
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        // key * d + channel within the page: the tile's first key may lie inside a page, and a page inside the tile
+        const int8_t* k = c.k + (int64_t(max(kpage[e], 0)) * c.heads + head) * B * d;
+        const int key = (tile * KT + kkey[e]) & in_page;
+        kc[e] = *reinterpret_cast<const uint4*>(k + key * d + (kat[e] - kkey[e] * d));
+        const int8_t* v = c.v + (int64_t(max(vpage[e], 0)) * c.heads + head) * B * d;
+        vc[e] = *reinterpret_cast<const uint4*>(v + vat[e] + ((tile * KT + vrun[e]) & in_page));
+      }
+      const int64_t s = int64_t(max(spage, 0)) * c.heads + head;
+      ks = c.kscale[s];
+      vs = c.vscale[s];
+      hole = spage < 0;
     }
-    const int64_t s = int64_t(max(spage, 0)) * c.heads + head;
-    ks = c.kscale[s];
-    vs = c.vscale[s];
-    hole = spage < 0;
   };
   auto put = [&](half8_t* to) {
 #pragma unroll
@@ -192,51 +212,61 @@ __global__ __launch_bounds__(kThreads, many_waves(Tag::dtype, DB)) void attend_m
 #pragma unroll
           for (int t = 0; t < QT; ++t) x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[e][t][s], x[t], 0, 0, 0);
       }
-      // the two runs of 16 keys: results 0 .. 7 and 8 .. 15
-      ValueScale sc[2];
-      float ksc[2];
-      bool gone[2], odd = key0 < all_lo || key0 + 32 > all_hi;
+      // runs of 16 keys, results 0 .. 7 and 8 .. 15, which may be of two pages
+      constexpr int kRuns = ONE ? 1 : 2, kRun = 16 / kRuns;
+      ValueScale sc[kRuns];
+      float ksc[kRuns];
+      bool gone[kRuns], odd = key0 < all_lo || key0 + 32 > all_hi;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        ksc[k] = lane_value(tks, 2 * n + k);
-        sc[k] = value_scale(lane_value(tvs, 2 * n + k));
-        gone[k] = __builtin_amdgcn_readlane(int(thole), 2 * n + k);
+      for (int k = 0; k < kRuns; ++k) {
+        const int at = ONE ? 0 : 2 * n + k;
+        ksc[k] = lane_value(tks, at);
+        sc[k] = value_scale(lane_value(tvs, at));
+        gone[k] = __builtin_amdgcn_readlane(int(thole), at);
         odd |= gone[k] || sc[k].zero || !(ksc[k] >= 0.f);
+        if constexpr (!kF32) {
+          // the mantissa goes into the exponent too: one rounding of the argument for the page, for a multiplication a weight
+          sc[k].exp += __builtin_amdgcn_logf(sc[k].mant);
+          sc[k].inv *= __builtin_amdgcn_rcpf(sc[k].mant);
+        }
       }
       half8_t wt[kParts][QT][2];
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
-        float f[2] = {unit[t] * ksc[0], unit[t] * ksc[1]};
-        if (a.softcap > 0.f) {
-          const float in = 1.f / a.softcap, out = a.softcap * kLog2e;
+        float f[kRuns];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[t][e] = capped<kF32>(x[t][e] * (f[e >> 3] * in), out);
-          f[0] = f[1] = 1.f;
+        for (int k = 0; k < kRuns; ++k) f[k] = unit[t] * ksc[k];
+        if (a.softcap > 0.f) {
+          const float in = kF32 ? 1.f / a.softcap : 2.f * kLog2e * __builtin_amdgcn_rcpf(a.softcap), out = a.softcap * kLog2e;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[t][e] = capped<kF32>(x[t][e] * (f[e / kRun] * in), out);
+#pragma unroll
+          for (int k = 0; k < kRuns; ++k) f[k] = 1.f;
         }
         float top = kNoKey;
         const int from = klo[t] - key0 - 4 * h, to = khi[t] - key0 - 4 * h;
-        auto in = [&](int e) { return bool(int(8 * (e >> 2) + (e & 3) >= from) & int(8 * (e >> 2) + (e & 3) < to) & int(!gone[e >> 3])); };
+        auto in = [&](int e) { return bool(int(8 * (e >> 2) + (e & 3) >= from) & int(8 * (e >> 2) + (e & 3) < to) & int(!gone[e / kRun])); };
         if (!odd) {
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            float y = x[t][8 * k];
+          for (int k = 0; k < kRuns; ++k) {
+            float y = x[t][kRun * k];
 #pragma unroll
-            for (int e = 1; e < 8; ++e) y = fmaxf(y, x[t][8 * k + e]);
-            top = fmaxf(top, y * f[k] + sc[k].exp);
+            for (int e = 1; e < kRun; ++e) y = fmaxf(y, x[t][kRun * k + e]);
+            top = fmaxf(top, fmaf(y, f[k], sc[k].exp));
           }
         } else {
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
+          for (int k = 0; k < kRuns; ++k) {
             float y = kNoKey;
 #pragma unroll
-            for (int e = 8 * k; e < 8 * k + 8; ++e) y = in(e) ? fmaxf(y, x[t][e] * f[k]) : y;
+            for (int e = kRun * k; e < kRun * k + kRun; ++e) y = in(e) ? fmaxf(y, x[t][e] * f[k]) : y;
             if (sc[k].zero) {
               // keys of a page of zeros count in the sum of weights only, on a maximum of their own
               const float most = fmaxf(mz[t], other_half(y));
               lz[t] *= __builtin_amdgcn_exp2f(mz[t] - most);
               mz[t] = most;
 #pragma unroll
-              for (int e = 8 * k; e < 8 * k + 8; ++e) lz[t] += in(e) ? __builtin_amdgcn_exp2f(x[t][e] * f[k] - most) : 0.f;
+              for (int e = kRun * k; e < kRun * k + kRun; ++e) lz[t] += in(e) ? __builtin_amdgcn_exp2f(x[t][e] * f[k] - most) : 0.f;
             } else {
               top = y == kNoKey ? top : fmaxf(top, y + sc[k].exp);
             }
@@ -252,25 +282,26 @@ __global__ __launch_bounds__(kThreads, many_waves(Tag::dtype, DB)) void attend_m
         }
         float P[16];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < kRuns; ++k) {
           const float shift = sc[k].exp - M[t];
           float sum = 0.f;
 #pragma unroll
-          for (int e = 8 * k; e < 8 * k + 8; ++e) P[e] = __builtin_amdgcn_exp2f(fmaf(x[t][e], f[k], shift));
-          if (odd) {
-#pragma unroll
-            for (int e = 8 * k; e < 8 * k + 8; ++e) P[e] = int(in(e)) & int(!sc[k].zero) ? P[e] : 0.f;
-          }
-#pragma unroll
-          for (int e = 8 * k; e < 8 * k + 8; ++e) {
-            sum += P[e];
-            P[e] *= sc[k].mant;
-          }
+          for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] = __builtin_amdgcn_exp2f(fmaf(x[t][e], f[k], shift));
           if (odd) {      // a scale that is no number must not reach keys that do not count
 #pragma unroll
-            for (int e = 8 * k; e < 8 * k + 8; ++e) P[e] = int(in(e)) & int(!sc[k].zero) ? P[e] : 0.f;
+            for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] = int(in(e)) & int(!sc[k].zero) ? P[e] : 0.f;
           }
-          l[t] = fmaf(sum, sc[k].inv, l[t]);
+#pragma unroll
+          for (int e = kRun * k; e < kRun * k + kRun; ++e) sum += P[e];
+          if constexpr (kF32) {
+#pragma unroll
+            for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] *= sc[k].mant;
+            if (odd) {
+#pragma unroll
+              for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] = int(in(e)) & int(!sc[k].zero) ? P[e] : 0.f;
+            }
+          }
+          l[t] = sum == 0.f ? l[t] : fmaf(sum, sc[k].inv, l[t]);      // (nothing times a scale that is no number is nothing)
         }
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
@@ -352,11 +383,11 @@ __global__ __launch_bounds__(kThreads) void attend_many_join_kernel(const Attend
   store_row<Tag>(p, r, first + row, head, ch, v, big, total);
 }
 
-template <class Tag, int DB, bool EXACT>
-int launch(const AttendPlan& p, hipStream_t st) {
+template <class Tag, int DB, bool EXACT, bool ONE>
+int launch_one(const AttendPlan& p, hipStream_t st) {
   constexpr int QT = many_tiles(Tag::dtype, DB), KT = many_keys(DB), kTile = 32 * QT * kWaves;
   constexpr size_t lds = 2 * 16 * (2 * 4 * DB * (KT + 1) + 2 * (KT / 16) * (64 * DB + 1));
-  const auto kern = attend_many_kernel<Tag, DB, EXACT, QT>;
+  const auto kern = attend_many_kernel<Tag, DB, EXACT, ONE, QT>;
   if (lds > 65536) {
     static const bool ok = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds)) == hipSuccess;
     if (!ok) return CAFEQ_ERR_LAUNCH;
@@ -371,6 +402,11 @@ int launch(const AttendPlan& p, hipStream_t st) {
     CAFEQ_CHECK_LAUNCH();
   }
   return CAFEQ_OK;
+}
+
+template <class Tag, int DB, bool EXACT>
+int launch(const AttendPlan& p, hipStream_t st) {
+  return p.c.block >= many_keys(DB) ? launch_one<Tag, DB, EXACT, true>(p, st) : launch_one<Tag, DB, EXACT, false>(p, st);
 }
 
 template <class Tag>
