@@ -98,10 +98,12 @@ __device__ __forceinline__ QueryScale query_scale(uint32_t bits, const cafeq_att
   return s;
 }
 
-// Many rows: keys of a tile, tiles of 32 rows a wave; what registers and LDS hold
-constexpr int many_keys(int db) { return db > 2 ? 32 : 64; }
-constexpr int many_tiles(int dtype, int db) { return 1; }
-constexpr int many_waves(int dtype, int db) { return dtype == CAFEQ_F32 && db > 2 ? 1 : 2; }
+// Many rows, by 64 channels (db): keys of a tile, waves of a workgroup (32 rows each), waves a SIMD that registers and LDS allow.  A prompt of 8192, TFLOP/s:
+// 8 heads of 256, 4 waves and 32 keys 675, 8 and 32 817, 8 and 64 856; 16 heads of 128, 4 and 64 817, 8 and 64 849, 4 and 32 (three waves a SIMD) 861, 8 and 128 784;
+// 4 heads of 64, 4 and 64 637, 8 and 64 569; in float32 16 heads of 128, 4 and 32 438, 4 and 64 450, 8 and 64 491.
+constexpr int many_keys(int dtype, int db) { return db == 2 && dtype != CAFEQ_F32 ? 32 : dtype == CAFEQ_F32 && db > 2 ? 32 : 64; }
+constexpr int many_waves(int dtype, int db) { return dtype == CAFEQ_F32 ? (db == 2 ? 8 : 4) : db > 2 ? 8 : 4; }
+constexpr int many_resident(int dtype, int db) { return dtype == CAFEQ_F32 ? (db > 2 ? 1 : 2) : db == 1 ? 4 : db == 2 ? 3 : 2; }
 
 struct AttendPlan {
   cafeq_cache c;

@@ -22,7 +22,9 @@ int check_attention(const cafeq_cache* c, const cafeq_attention* a) {
   return CAFEQ_OK;
 }
 
-constexpr int64_t kFewRows = 64;
+// Rows of a sequence and key head up to which attend_few is the faster, though it reads the keys once for every 16: 8 x 3000 keys of 16 heads of 128, 64 rows,
+// 79 us in four tiles of 16 and 60 by attend_many; of 8 heads of 256 64 and 81; 60000 keys of 8 heads of 256, 32 rows 75 and 150, 128 rows 239 and 172.
+int64_t few_rows(const cafeq_cache& c) { return c.d > 128 ? 64 : 32; }
 
 size_t sums_bytes(const AttendPlan& p, int64_t tiles) {
   return p.splits > 1 ? align_up(size_t(tiles) * p.c.heads * p.splits * p.keep * 2 * sizeof(float), 256) : 0;
@@ -62,14 +64,15 @@ AttendPlan plan_few(const cafeq_cache& c, const cafeq_attention& a, int64_t rows
 
 AttendPlan plan_many(const cafeq_cache& c, const cafeq_attention& a, int64_t few_rows, int64_t room) {
   AttendPlan p{c, a, a.heads_q / c.heads, __builtin_ctz(unsigned(c.block))};
-  const int db = (c.d + 63) / 64, tile = 128 * many_tiles(a.dtype, db), kt = many_keys(db);
+  const int db = (c.d + 63) / 64, tile = 32 * many_waves(a.dtype, db), kt = many_keys(a.dtype, db);
   p.few_rows = int(few_rows);
   p.units = Units{p.rep, tile, 1};
   p.keep = tile;
   const int64_t keys = a.window > 0 && a.causal ? std::min(room, a.window + tile / p.rep + int64_t(2 * kt)) : room;
   const int64_t groups = p.units.count(a.n, c.sequences) * c.heads;
-  // two workgroups a compute unit, none with less than 512 keys
-  const int64_t want = std::min((512 + groups - 1) / groups, (keys + 511) / 512);
+  // workgroups for what the chip holds at once, none with less than 512 keys
+  const int64_t slots = int64_t(device_cu_count()) * many_resident(a.dtype, db) * 4 / many_waves(a.dtype, db);
+  const int64_t want = std::min((slots + groups - 1) / groups, (keys + 511) / 512);
   p.span = int((keys + want * kt - 1) / (want * kt));
   p.splits = int((keys + int64_t(p.span) * kt - 1) / (int64_t(p.span) * kt));
   return p;
@@ -80,16 +83,17 @@ AttendPlans plan(const cafeq_cache& c, const cafeq_attention& given) {
   cafeq_attention a = given;
   a.longest = std::min(a.longest, a.n);
   const int64_t rep = a.heads_q / c.heads, rows = a.longest * rep, room = int64_t(c.width) * c.block;
-  s.many = rows > kFewRows;
+  const int64_t few = few_rows(c);
+  s.many = rows > few;
   s.few = !s.many || c.sequences > 1;
   if (s.few) {
-    s.f = plan_few(c, a, std::min(rows, kFewRows), room);
+    s.f = plan_few(c, a, std::min(rows, few), room);
     s.few_tiles = int64_t(c.sequences) * s.f.tiles;
     s.few_sums = sums_bytes(s.f, s.few_tiles);
     s.few_parts = parts_bytes(s.f, s.few_tiles);
   }
   if (s.many) {
-    s.m = plan_many(c, a, s.few ? kFewRows : 0, room);
+    s.m = plan_many(c, a, s.few ? few : 0, room);
     s.many_tiles = s.m.units.count(a.n, c.sequences);
     s.many_sums = sums_bytes(s.m, s.many_tiles);
     s.many_parts = parts_bytes(s.m, s.many_tiles);

@@ -5,7 +5,7 @@
 namespace cafeq {
 namespace {
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kJoin = 256;
 
 __device__ __forceinline__ float other_half(float v) {
   const uint32_t u = __float_as_uint(v);
@@ -14,17 +14,17 @@ __device__ __forceinline__ float other_half(float v) {
 }
 __device__ __forceinline__ float lane_value(float v, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); }
 
-// A workgroup: 128 QT rows, 32 QT a wave, over a part of the keys, in tiles of KT.  A tile's codes are read once, become float16 on their way to LDS
+// A workgroup: 32 rows a wave, over a part of the keys, in tiles of KT.  A tile's codes are read once, become float16 on their way to LDS
 // and are what all waves multiply: v_mfma 32x32x16, S^T = K Q^T with the rows of q in registers, then out^T = V^T P^T.  Lane l holds row l % 32,
 // and of 32 keys those with key / 4 % 2 = l / 32: results i of a product are keys 8 (i / 4) + 4 (l / 32) + i % 4, weights 8 u .. 8 u + 7 what it gives to step u of
 // the second product.  LDS: K as [16 channels][half][key], V as [16 keys][half][channel] of eight float16 each, a place of 16 bytes
 // behind every run so that lanes that write side by side hit different banks.  Two buffers: the next tile's codes are on their way while this one is multiplied.
 // ONE: a tile's keys are of one page.
-template <class Tag, int DB, bool EXACT, bool ONE, int QT>
-__global__ __launch_bounds__(kThreads, many_waves(Tag::dtype, DB)) void attend_many_kernel(const AttendPlan p) {
+template <class Tag, int DB, bool EXACT, bool ONE>
+__global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag::dtype, DB)) void attend_many_kernel(const AttendPlan p) {
   using elem = typename Tag::elem;
   constexpr bool kF32 = Tag::dtype == CAFEQ_F32;
-  constexpr int kParts = kF32 ? 2 : 1, KT = many_keys(DB), NT = KT / 32, KS = 4 * DB, MT = 2 * DB, U = KT / 16;
+  constexpr int QT = 1, kWaves = many_waves(Tag::dtype, DB), kThreads = 64 * kWaves, kParts = kF32 ? 2 : 1, KT = many_keys(Tag::dtype, DB), NT = KT / 32, KS = 4 * DB, MT = 2 * DB, U = KT / 16;
   constexpr int kTile = 32 * QT * kWaves, E = (KT * KS + kThreads - 1) / kThreads;
   constexpr int kRunK = KT + 1, kRunV = 64 * DB + 1, kBufK = 2 * KS * kRunK, kBuf = kBufK + 2 * U * kRunV;
   extern __shared__ __align__(16) half8_t buf[];
@@ -354,9 +354,9 @@ __global__ __launch_bounds__(kThreads, many_waves(Tag::dtype, DB)) void attend_m
 }
 
 // The parts of a tile's rows joined in their order, four channels a thread.
-template <class Tag, int DB, int QT>
-__global__ __launch_bounds__(kThreads) void attend_many_join_kernel(const AttendPlan p) {
-  constexpr int kTile = 32 * QT * kWaves, KT = many_keys(DB);
+template <class Tag, int DB>
+__global__ __launch_bounds__(kJoin) void attend_many_join_kernel(const AttendPlan p) {
+  constexpr int kTile = 32 * many_waves(Tag::dtype, DB), KT = many_keys(Tag::dtype, DB);
   const cafeq_cache& c = p.c;
   const int head = blockIdx.x % c.heads, d = c.d, per = d / 4;
   const int64_t w = blockIdx.x / c.heads;
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(kThreads) void attend_many_join_kernel(const Attend
   const Reach r = reach_of(c, p.a, i, p.rep, first, kTile);
   if (first >= r.rows || r.rows <= p.few_rows) return;
   const int c0 = r.lo / KT, c1 = max(c0, (r.hi + KT - 1) / KT), used = (c1 - c0 + p.span - 1) / p.span;
-  const int e = blockIdx.y * kThreads + threadIdx.x, row = e / per, ch = e % per * 4;
+  const int e = blockIdx.y * kJoin + threadIdx.x, row = e / per, ch = e % per * 4;
   if (used <= 1 || row >= kTile || first + row >= r.rows) return;
   const int64_t part = (w * c.heads + head) * p.splits * kTile + row;
   float big = kNoKey, total = 0.f;
@@ -385,20 +385,20 @@ __global__ __launch_bounds__(kThreads) void attend_many_join_kernel(const Attend
 
 template <class Tag, int DB, bool EXACT, bool ONE>
 int launch_one(const AttendPlan& p, hipStream_t st) {
-  constexpr int QT = many_tiles(Tag::dtype, DB), KT = many_keys(DB), kTile = 32 * QT * kWaves;
+  constexpr int KT = many_keys(Tag::dtype, DB), kWaves = many_waves(Tag::dtype, DB), kTile = 32 * kWaves;
   constexpr size_t lds = 2 * 16 * (2 * 4 * DB * (KT + 1) + 2 * (KT / 16) * (64 * DB + 1));
-  const auto kern = attend_many_kernel<Tag, DB, EXACT, ONE, QT>;
+  const auto kern = attend_many_kernel<Tag, DB, EXACT, ONE>;
   if (lds > 65536) {
     static const bool ok = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds)) == hipSuccess;
     if (!ok) return CAFEQ_ERR_LAUNCH;
   }
   // the heads innermost: workgroups go round the eight XCDs in turn, so that a head's tiles stay behind one L2
   const unsigned units = unsigned(p.units.count(p.a.n, p.c.sequences) * p.c.heads);
-  hipLaunchKernelGGL(kern, dim3(units, unsigned(p.splits)), dim3(kThreads), lds, st, p);
+  hipLaunchKernelGGL(kern, dim3(units, unsigned(p.splits)), dim3(64 * kWaves), lds, st, p);
   CAFEQ_CHECK_LAUNCH();
   if (p.splits > 1) {
-    const unsigned y = unsigned((kTile * (p.c.d / 4) + kThreads - 1) / kThreads);
-    hipLaunchKernelGGL((attend_many_join_kernel<Tag, DB, QT>), dim3(units, y), dim3(kThreads), 0, st, p);
+    const unsigned y = unsigned((kTile * (p.c.d / 4) + kJoin - 1) / kJoin);
+    hipLaunchKernelGGL((attend_many_join_kernel<Tag, DB>), dim3(units, y), dim3(kJoin), 0, st, p);
     CAFEQ_CHECK_LAUNCH();
   }
   return CAFEQ_OK;
@@ -406,7 +406,7 @@ int launch_one(const AttendPlan& p, hipStream_t st) {
 
 template <class Tag, int DB, bool EXACT>
 int launch(const AttendPlan& p, hipStream_t st) {
-  return p.c.block >= many_keys(DB) ? launch_one<Tag, DB, EXACT, true>(p, st) : launch_one<Tag, DB, EXACT, false>(p, st);
+  return p.c.block >= many_keys(Tag::dtype, DB) ? launch_one<Tag, DB, EXACT, true>(p, st) : launch_one<Tag, DB, EXACT, false>(p, st);
 }
 
 template <class Tag>

@@ -149,30 +149,17 @@ struct ValueArgs {
   Units units;
 };
 
+// Slots f .. f + m - 1 of a page and head; row0: the row of slot 0; slots from `known` on, and those of a page that is not there, are zeros
 template <class Tag>
-__global__ __launch_bounds__(kThreads) void values_kernel(const ValueArgs a) {
+__device__ __forceinline__ void page_values(const ValueArgs& a, int side, int head, int page, int64_t row0, int f, int m, int known) {
   using elem = typename Tag::elem;
   const cafeq_cache& c = a.c;
-  const int head = blockIdx.y, side = blockIdx.z, tid = threadIdx.x, B = c.block, d = c.d;
-  if (!a.out[side]) return;
-  const int64_t w = blockIdx.x;
-  const int i = sequence_of(a.units, a.starts, c.sequences, a.n, w);
-  if (i < 0) return;
-  const RowRange r = rows_of(a.starts, i, a.n);
-  const int64_t pos0 = a.begin[i], rows = r.hi - r.lo, len = tokens_of(c, i);
-  // blocks of positions, counted from the one that holds begin (negative positions included)
-  const int64_t block = (pos0 >= 0 ? pos0 / B : -((-pos0 + B - 1) / B)) + (w - a.units.base(r.lo, i));
-  const int64_t first = max(pos0, block * B), last = min(pos0 + rows, (block + 1) * B);
-  if (first >= last) return;
-  const int page = first >= 0 && first < len ? page_of(c, i, int(block)) : -1;
+  const int tid = threadIdx.x, B = c.block, d = c.d, per = d / 8;
   const int64_t at = int64_t(max(page, 0)) * c.heads + head;
   const int8_t* codes = (side ? c.v : c.k) + at * B * d;
   const float s = page < 0 ? 0.f : (side ? c.vscale : c.kscale)[at];
-  // row of slot 0 of the page
-  elem* out = static_cast<elem*>(a.out[side]) + ((r.lo + block * B - pos0) * c.heads + head) * d;
-  const int f = int(first - block * B), m = int(last - first), per = d / 8;
+  elem* out = static_cast<elem*>(a.out[side]) + (row0 * c.heads + head) * d;
   const int64_t ld = int64_t(c.heads) * d;
-  const int known = page < 0 ? 0 : int(min(int64_t(B), len - block * B));      // slots behind it, and of pages that are not there: zeros
   auto store = [&](int slot, int ch, const float* v) {
     elem* o = out + slot * ld + ch;
     if constexpr (Tag::dtype == CAFEQ_F32) {
@@ -209,6 +196,26 @@ __global__ __launch_bounds__(kThreads) void values_kernel(const ValueArgs a) {
       store(slot + k, ch, v);
     }
   }
+}
+
+// A workgroup: what one page and head hold of a sequence's rows, keys or values.
+template <class Tag>
+__global__ __launch_bounds__(kThreads) void values_kernel(const ValueArgs a) {
+  const cafeq_cache& c = a.c;
+  const int side = blockIdx.z, B = c.block;
+  if (!a.out[side]) return;
+  const int64_t w = blockIdx.x;
+  const int i = sequence_of(a.units, a.starts, c.sequences, a.n, w);
+  if (i < 0) return;
+  const RowRange r = rows_of(a.starts, i, a.n);
+  const int64_t pos0 = a.begin[i], rows = r.hi - r.lo, len = tokens_of(c, i);
+  // blocks of positions, counted from the one that holds begin (negative positions included)
+  const int64_t block = (pos0 >= 0 ? pos0 / B : -((-pos0 + B - 1) / B)) + (w - a.units.base(r.lo, i));
+  const int64_t first = max(pos0, block * B), last = min(pos0 + rows, (block + 1) * B);
+  if (first >= last) return;
+  const int page = first >= 0 && first < len ? page_of(c, i, int(block)) : -1;
+  page_values<Tag>(a, side, int(blockIdx.y), page, r.lo + block * B - pos0, int(first - block * B), int(last - first),
+                   page < 0 ? 0 : int(min(int64_t(B), len - block * B)));
 }
 
 template <class Tag>

@@ -7,7 +7,7 @@ namespace cafeq {
 namespace {
 
 constexpr int kScan = 1024, kCopy = 256;
-constexpr int64_t kSmallTable = 16384;      // entries of a table that one workgroup reorders in 64 KB of LDS
+constexpr int64_t kSmallTable = 16384;      // words of LDS (64 KB) with which one workgroup reorders a table in one launch
 
 // Scratch of all three calls, int32 throughout
 struct PageWs {
@@ -126,8 +126,6 @@ __global__ __launch_bounds__(kScan) void reserve_kernel(const ReserveArgs a) {
       row[have + e] = list[extra + e];
       c.refs[list[extra + e]] = 1;
     }
-    if (a.positions)
-      for (int e = lane; e < more; e += 64) a.positions[r.lo + e] = len + e;
     // the wave has read the length before it is written: its lanes run in step
     if (lane == 0 && more > 0) c.lengths[i] = len + more;
   }
@@ -145,9 +143,18 @@ __device__ __forceinline__ void copy_item(const cafeq_cache& c, int from, int to
   if (threadIdx.x == 0) scale[dst] = scale[src];
 }
 
-__global__ __launch_bounds__(kCopy) void copy_shared_kernel(const cafeq_cache c, const PageWs w) {
+// The second part of reserve: positions of the new tokens, and copies
+__global__ __launch_bounds__(kCopy) void copy_shared_kernel(const ReserveArgs a) {
+  const cafeq_cache& c = a.c;
+  const PageWs& w = a.w;
   const int i = blockIdx.x;
-  if (w.head[0] != 0 || w.from[i] < 0) return;
+  if (w.head[0] != 0) return;
+  if (a.positions) {
+    const RowRange r = rows_of(a.starts, i, a.n);
+    const int before = c.lengths[i] - (r.hi - r.lo);
+    for (int e = r.lo + blockIdx.y * kCopy + threadIdx.x; e < r.hi; e += gridDim.y * kCopy) a.positions[e] = before + (e - r.lo);
+  }
+  if (w.from[i] < 0) return;
   for (int item = blockIdx.y; item < 2 * c.heads; item += gridDim.y) copy_item(c, w.from[i], w.to[i], item);
 }
 
@@ -176,21 +183,29 @@ __global__ __launch_bounds__(kCopy) void reorder_kernel(const cafeq_cache c, con
 
 // The same for a table that LDS holds: one workgroup, one launch.
 __global__ __launch_bounds__(kScan) void reorder_small_kernel(const cafeq_cache c, const int32_t* sources) {
-  extern __shared__ int32_t held[];      // the table, then the lengths
+  extern __shared__ int32_t held[];      // the table, then blocks of the rows, lengths and sources
   const int tid = threadIdx.x, total = c.sequences * c.width, B = c.block;
-  int32_t* lengths = held + total;
+  int32_t *blocks = held + total, *lengths = blocks + c.sequences, *from = lengths + c.sequences;
   for (int e = tid; e < total; e += kScan) held[e] = c.table[e];
-  for (int e = tid; e < c.sequences; e += kScan) lengths[e] = tokens_of(c, e);
+  for (int e = tid; e < c.sequences; e += kScan) {
+    lengths[e] = tokens_of(c, e);
+    blocks[e] = blocks_of(lengths[e], B);
+    const int s = sources[e];
+    from[e] = s >= 0 && s < c.sequences ? s : -1;
+  }
   __syncthreads();
-  for (int e = tid; e < total; e += kScan) {
-    const int i = e / c.width, b = e - i * c.width, from = sources[i];
-    if (from == i) continue;
-    const bool some = from >= 0 && from < c.sequences;
-    const int p = some && b < blocks_of(lengths[from], B) ? held[from * c.width + b] : -1, q = b < blocks_of(lengths[i], B) ? held[e] : -1;
-    c.table[e] = p;
-    if (p >= 0 && p < c.pages) atomicAdd(c.refs + p, 1);
-    if (q >= 0 && q < c.pages) atomicSub(c.refs + q, 1);
-    if (b == 0) c.lengths[i] = some ? lengths[from] : 0;
+  // a wave a row
+  for (int i = tid >> 6; i < c.sequences; i += kScan / 64) {
+    const int s = from[i];
+    if (s == i) continue;
+    const int mine = blocks[i], theirs = s < 0 ? 0 : blocks[s];
+    for (int b = tid & 63; b < c.width; b += 64) {
+      const int p = b < theirs ? held[s * c.width + b] : -1, q = b < mine ? held[i * c.width + b] : -1;
+      c.table[i * c.width + b] = p;
+      if (p >= 0 && p < c.pages) atomicAdd(c.refs + p, 1);
+      if (q >= 0 && q < c.pages) atomicSub(c.refs + q, 1);
+    }
+    if ((tid & 63) == 0) c.lengths[i] = s < 0 ? 0 : lengths[s];
   }
 }
 
@@ -204,16 +219,25 @@ __global__ __launch_bounds__(kScan) void plan_compact_kernel(const cafeq_cache c
   scan_before(count, &total);
   const int in_use = total;
   int moves = 0, holes = 0;
-  for (int64_t p0 = 0; p0 < c.pages; p0 += kScan) {
-    const int64_t p = p0 + tid;
-    const bool live = p < c.pages && c.refs[p] > 0;
-    const int move = live && p >= in_use, hole = p < in_use && !live;
-    const int at = moves + scan_before(move, &total);
-    if (move) w.list[at] = int(p);
-    moves += total;
-    const int to = holes + scan_before(hole, &total);
-    if (hole) w.list2[to] = int(p);
-    holes += total;
+  for (int64_t p0 = 0; p0 < c.pages; p0 += 4 * kScan) {
+    int move = 0, hole = 0;      // of the thread's four pages, by bits
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int64_t p = p0 + 4 * tid + e;
+      const bool live = p < c.pages && c.refs[p] > 0;
+      move |= int(live && p >= in_use) << e;
+      hole |= int(p < in_use && !live) << e;
+    }
+    // both counts in one sum: a step has at most 4096 of either
+    const int before = scan_before(__popc(move) | __popc(hole) << 16, &total);
+    int at = moves + (before & 0xFFFF), to = holes + (before >> 16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (move >> e & 1) w.list[at++] = int(p0 + 4 * tid + e);
+      if (hole >> e & 1) w.list2[to++] = int(p0 + 4 * tid + e);
+    }
+    moves += total & 0xFFFF;
+    holes += total >> 16;
   }
   if (tid == 0) {
     *used = in_use;
@@ -276,7 +300,7 @@ int cafeq_cache_reserve(const cafeq_cache* cache, const int32_t* starts, int64_t
   CAFEQ_CHECK_LAUNCH();
   if (cache->sequences == 0 || n == 0) return CAFEQ_OK;
   const int y = std::max(1, std::min(2 * cache->heads, 65536 / std::max(1, cache->sequences)));
-  hipLaunchKernelGGL(copy_shared_kernel, dim3(unsigned(cache->sequences), unsigned(y)), dim3(kCopy), 0, st, *cache, a.w);
+  hipLaunchKernelGGL(copy_shared_kernel, dim3(unsigned(cache->sequences), unsigned(y)), dim3(kCopy), 0, st, a);
   CAFEQ_CHECK_LAUNCH();
   return CAFEQ_OK;
 }
@@ -290,8 +314,9 @@ int cafeq_cache_reorder(const cafeq_cache* cache, const int32_t* sources, void* 
   hipStream_t st = static_cast<hipStream_t>(stream);
   const PageWs w = page_ws(*cache, ws);
   const int64_t entries = int64_t(cache->sequences) * cache->width;
-  if (entries + cache->sequences <= kSmallTable) {
-    hipLaunchKernelGGL(reorder_small_kernel, dim3(1), dim3(kScan), size_t(entries + cache->sequences) * sizeof(int32_t), st, *cache, sources);
+  const int64_t words = entries + 3 * int64_t(cache->sequences);
+  if (words <= kSmallTable) {
+    hipLaunchKernelGGL(reorder_small_kernel, dim3(1), dim3(kScan), size_t(words) * sizeof(int32_t), st, *cache, sources);
     CAFEQ_CHECK_LAUNCH();
     return CAFEQ_OK;
   }

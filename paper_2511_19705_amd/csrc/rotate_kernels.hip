@@ -88,8 +88,8 @@ __device__ __forceinline__ void put(uint16_t* p, const float* v) {
 }
 
 // A cluster of LANES lanes holds a head, each lane IT runs of VP pairs of channels: it forms the sines of its pairs once for the token and
-// goes over the heads.  Runs behind the turned ones are 2 VP neighbouring channels that stay.
-template <class Tag, int VP, int LANES, int IT>
+// goes over the heads, NH of them requested at once.  Runs behind the turned ones are 2 VP neighbouring channels that stay.
+template <class Tag, int VP, int LANES, int IT, int NH>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
   using elem = typename Tag::elem;
   constexpr int kClusters = kThreads / LANES;
@@ -97,90 +97,118 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
   const int step = gridDim.y * kClusters, heads = a.part[0].heads + a.part[1].heads;
   const int64_t t = blockIdx.x;
   const int half = a.c.rot / 2, turned = half / VP, runs = a.c.d / 2 / VP;
-  float cs[IT][VP], sn[IT][VP];
-  const double pos = a.positions[t];
   int at[IT], gap[IT];     // first channel of a run, and how far the pairs' partners lie (0: 2 VP channels side by side)
 #pragma unroll
   for (int i = 0; i < IT; ++i) {
     const int r = lane + LANES * i;
     at[i] = r < turned && !a.c.interleaved ? r * VP : r * 2 * VP;
     gap[i] = r < turned && !a.c.interleaved ? half : 0;
+  }
+  float v[NH][IT][2 * VP];
+  auto request = [&](int h0) {
+#pragma unroll
+    for (int k = 0; k < NH; ++k) {
+      const int hh = h0 + k * step;
+      const bool second = hh >= a.part[0].heads;
+      const cafeq_heads& p = a.part[second];
+      const elem* x = static_cast<const elem*>(p.x) + t * p.ldx + (second ? hh - a.part[0].heads : hh) * p.hsx;
+#pragma unroll
+      for (int i = 0; i < IT; ++i) {
+        if (hh < heads && lane + LANES * i < runs) {
+          if (gap[i]) {
+            get<VP>(x + at[i], v[k][i]);
+            get<VP>(x + at[i] + gap[i], v[k][i] + VP);
+          } else {
+            get<2 * VP>(x + at[i], v[k][i]);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 2 * VP; ++e) v[k][i][e] = 0.f;
+        }
+      }
+    }
+  };
+  request(cluster);
+  // The sines once for the workgroup.  Revolutions, whole ones taken off in float64; of the rest sincospi is good to float32's last bits, the hardware's
+  // sine to 2^-20, which is 2^-12 of a step of bfloat16
+  __shared__ __align__(16) float cos_lds[kHeadMax / 2], sin_lds[kHeadMax / 2];
+  if (threadIdx.x < half) {
+    const double rev = a.positions[t] * 0.15915494309189533577 * a.freq[threadIdx.x];
+    const float rest = float(rev - rint(rev));
+    float s, c;
+    if constexpr (Tag::dtype == CAFEQ_F32) {
+      sincospif(2.f * rest, &s, &c);
+    } else {
+      s = __builtin_amdgcn_sinf(rest);
+      c = __builtin_amdgcn_cosf(rest);
+    }
+    cos_lds[threadIdx.x] = c * a.c.amplitude;
+    sin_lds[threadIdx.x] = s * a.c.amplitude;
+  }
+  __syncthreads();
+  float cs[IT][VP], sn[IT][VP];
+#pragma unroll
+  for (int i = 0; i < IT; ++i) {
+    const int r = lane + LANES * i;
+    if (r >= turned) continue;
 #pragma unroll
     for (int e = 0; e < VP; ++e) {
-      cs[i][e] = 1.f;
-      sn[i][e] = 0.f;
-      if (r < turned) {
-        // revolutions, whole ones taken off in float64; sincospi of twice the rest is good to float32's last bits
-        const double rev = pos * a.freq[r * VP + e] * 0.15915494309189533577;
-        float s, c;
-        sincospif(float(2.0 * (rev - rint(rev))), &s, &c);
-        cs[i][e] = c * a.c.amplitude;
-        sn[i][e] = s * a.c.amplitude;
-      }
+      cs[i][e] = cos_lds[r * VP + e];
+      sn[i][e] = sin_lds[r * VP + e];
     }
   }
-  for (int h0 = cluster; h0 < heads; h0 += step) {
-    const bool second = h0 >= a.part[0].heads;
-    const cafeq_heads& p = a.part[second];
-    const int h = second ? h0 - a.part[0].heads : h0;
-    const elem* x = static_cast<const elem*>(p.x) + t * p.ldx + h * p.hsx;
-    elem* o = static_cast<elem*>(p.out) + t * p.ldo + h * p.hso;
-    float v[IT][2 * VP], sum = 0.f;
+  for (int h0 = cluster; h0 < heads;) {
 #pragma unroll
-    for (int i = 0; i < IT; ++i) {
-      if (lane + LANES * i < runs) {
-        if (gap[i]) {
-          get<VP>(x + at[i], v[i]);
-          get<VP>(x + at[i] + gap[i], v[i] + VP);
-        } else {
-          get<2 * VP>(x + at[i], v[i]);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 2 * VP; ++e) v[i][e] = 0.f;
-      }
-#pragma unroll
-      for (int e = 0; e < 2 * VP; ++e) sum += v[i][e] * v[i][e];
-    }
-    float scale = 1.f;
-    if (a.c.norm) scale = 1.f / sqrtf(cluster_sum<LANES>(sum) / float(a.c.d) + a.c.eps);
-#pragma unroll
-    for (int i = 0; i < IT; ++i) {
-      if (lane + LANES * i >= runs) continue;
+    for (int k = 0; k < NH; ++k) {
+      const int hh = h0 + k * step;
+      if (hh >= heads) continue;
+      const bool second = hh >= a.part[0].heads;
+      const cafeq_heads& p = a.part[second];
+      elem* o = static_cast<elem*>(p.out) + t * p.ldo + (second ? hh - a.part[0].heads : hh) * p.hso;
+      float scale = 1.f;
       if (a.c.norm) {
-        float g[2 * VP];
-        if (p.gain && gap[i]) {
-          get<VP>(p.gain + at[i], g);
-          get<VP>(p.gain + at[i] + gap[i], g + VP);
-        } else if (p.gain) {
-          get<2 * VP>(p.gain + at[i], g);
-        }
+        float sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < 2 * VP; ++e) v[i][e] = v[i][e] * scale * (p.gain ? a.c.gain_offset + g[e] : 1.f);
+        for (int i = 0; i < IT; ++i)
+#pragma unroll
+          for (int e = 0; e < 2 * VP; ++e) sum += v[k][i][e] * v[k][i][e];
+        scale = 1.f / sqrtf(cluster_sum<LANES>(sum) / float(a.c.d) + a.c.eps);
       }
-      if (lane + LANES * i < turned) {
 #pragma unroll
-        for (int e = 0; e < VP; ++e) {
-          // the pair's places in v
-          const int ia = e, ib = VP + e, ja = 2 * e, jb = 2 * e + 1;
-          if (gap[i]) {
-            const float x0 = v[i][ia], x1 = v[i][ib];
-            v[i][ia] = x0 * cs[i][e] - x1 * sn[i][e];
-            v[i][ib] = x0 * sn[i][e] + x1 * cs[i][e];
-          } else {
-            const float x0 = v[i][ja], x1 = v[i][jb];
-            v[i][ja] = x0 * cs[i][e] - x1 * sn[i][e];
-            v[i][jb] = x0 * sn[i][e] + x1 * cs[i][e];
+      for (int i = 0; i < IT; ++i) {
+        if (lane + LANES * i >= runs) continue;
+        float(&x)[2 * VP] = v[k][i];
+        if (a.c.norm) {
+          float g[2 * VP];
+          if (p.gain && gap[i]) {
+            get<VP>(p.gain + at[i], g);
+            get<VP>(p.gain + at[i] + gap[i], g + VP);
+          } else if (p.gain) {
+            get<2 * VP>(p.gain + at[i], g);
+          }
+#pragma unroll
+          for (int e = 0; e < 2 * VP; ++e) x[e] = x[e] * scale * (p.gain ? a.c.gain_offset + g[e] : 1.f);
+        }
+        if (lane + LANES * i < turned) {
+#pragma unroll
+          for (int e = 0; e < VP; ++e) {
+            // the pair's places
+            float &x0 = gap[i] ? x[e] : x[2 * e], &x1 = gap[i] ? x[VP + e] : x[2 * e + 1];
+            const float y0 = x0, y1 = x1;
+            x0 = y0 * cs[i][e] - y1 * sn[i][e];
+            x1 = y0 * sn[i][e] + y1 * cs[i][e];
           }
         }
-      }
-      if (gap[i]) {
-        put<VP>(o + at[i], v[i]);
-        put<VP>(o + at[i] + gap[i], v[i] + VP);
-      } else {
-        put<2 * VP>(o + at[i], v[i]);
+        if (gap[i]) {
+          put<VP>(o + at[i], x);
+          put<VP>(o + at[i] + gap[i], x + VP);
+        } else {
+          put<2 * VP>(o + at[i], x);
+        }
       }
     }
+    h0 += NH * step;
+    if (h0 < heads) request(h0);
   }
 }
 
@@ -189,7 +217,7 @@ int launch(const RotateArgs& a, hipStream_t st) {
   const int heads = a.part[0].heads + a.part[1].heads, per = kThreads / LANES;
   // few tokens: the heads over several workgroups; many: one a token, whose sines serve all its heads
   const int y = a.n >= 256 ? 1 : (heads + per - 1) / per;
-  hipLaunchKernelGGL((rotate_kernel<Tag, VP, LANES, IT>), dim3(unsigned(a.n), unsigned(y)), dim3(kThreads), 0, st, a);
+  hipLaunchKernelGGL((rotate_kernel<Tag, VP, LANES, IT, (IT > 1 ? 1 : 4)>), dim3(unsigned(a.n), unsigned(y)), dim3(kThreads), 0, st, a);
   CAFEQ_CHECK_LAUNCH();
   return CAFEQ_OK;
 }
