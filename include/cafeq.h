@@ -310,7 +310,7 @@ int cafeq_rotate_heads(const cafeq_rotation* cfg, const cafeq_heads* q, const ca
  * [sequences][width]: the page of each block of a sequence (blocks behind its length: -1); lengths [sequences]: its tokens;
  * refs [pages]: rows of the table that hold a page (0: free; used by reserve, reorder and compact only).  All device memory, owned by the
  * caller; k and v 16-byte aligned.  d a multiple of 16 up to 256, block 16, 32, 64 or 128, pages * heads up to 2^31 - 1, heads up to 4096,
- * width * block below 2^31, sequences up to 65535.  Numbers in device memory are not trusted with addresses: lengths beyond width * block count as
+ * width * block up to 2^30, sequences up to 65535.  Numbers in device memory are not trusted with addresses: lengths beyond width * block count as
  * that, and tokens whose page is outside [0, pages) are not read or written and are no keys. */
 typedef struct {
   int8_t* k;
@@ -345,7 +345,7 @@ int cafeq_cache_values(const cafeq_cache* cache, const int32_t* begin, const int
  * head h reads key head h / (heads_q / heads):
  *   x_t = scale q . K_t, with softcap > 0: softcap tanh(x_t / softcap);  keys t: 0 <= t < lengths[i], t <= p if causal, t > p - window if window > 0
  *   out = sum_t exp(x_t) V_t / sum_t exp(x_t),  lse = log sum_t exp(x_t)   (a row without keys: 0 and -inf)
- * K, V: the codes times their scales.  q, out float32 or bfloat16 (dtype); lse float32 [n][heads_q] dense or NULL.  Queries of bfloat16 are
+ * K, V: the codes times their scales, which are not negative.  q, out float32 or bfloat16 (dtype); lse float32 [n][heads_q] dense or NULL.  Queries of bfloat16 are
  * taken exactly (magnitudes below 2^-28 of the row's largest to multiples of 2^-39 of it), probabilities rounded to 11 bits (below 2^-28 of the
  * largest, weighed with the scale of v, to multiples of 2^-39 of it); with float32 both are taken in two such parts.  Sums are float32 in a fixed order.  A row of q that holds a NaN or an infinity gives NaN.  A page and head of v with a scale below 2^-100 counts as zeros.
  * Rows start at multiples of 16 bytes; out overlaps no input.  longest as in cafeq_cache_append (rows beyond it are left).

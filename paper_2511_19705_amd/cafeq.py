@@ -800,7 +800,7 @@ def rotate_heads(q, k, positions, freq, interleaved=False, norm=False, gain_q=No
 
 class KVCache:
     """A cache as cafeq.h describes it: codes and scales of keys and values, the page of each block of a sequence, tokens of a sequence, rows that
-    hold a page.  Its tensors are checked at the first call and after one of them was replaced; their contents may change at will."""
+    hold a page.  Its tensors are checked at the first call and after one of them was replaced or moved; their contents may change at will."""
     __slots__ = ("k", "v", "kscale", "vscale", "table", "lengths", "refs", "_desc")
     _fields = __slots__[:7]
 
@@ -830,9 +830,12 @@ def kv_cache(sequences, pages, heads, d, block=64, width=None, device=None):
 
 
 def _cache(c, dev):
-    """(descriptor, its reference for a call) of a KVCache on device number `dev`.  What the seven checks cost (8 us) is paid once."""
+    """(descriptor, its reference for a call, device, scratch of the page calls, addresses) of a KVCache on device number `dev`.  The checks of seven
+    tensors (8 us) are made once, and again where one has another address, or k or the table another shape."""
     have = c._desc
-    if have is not None and have[2] == dev:
+    at = (c.k.data_ptr(), c.v.data_ptr(), c.kscale.data_ptr(), c.vscale.data_ptr(), c.table.data_ptr(), c.lengths.data_ptr(), c.refs.data_ptr(), c.k.shape,
+          c.table.shape)
+    if have is not None and have[2] == dev and have[4] == at:
         return have
     if len(c.k.shape) != 4 or len(c.table.shape) != 2:
         raise CafeqError("cache: k must be [pages][heads][block][d], table [sequences][width]")
@@ -843,7 +846,7 @@ def _cache(c, dev):
                  _operand(c.kscale, dev, f32, (pages, heads), "cache.kscale"), _operand(c.vscale, dev, f32, (pages, heads), "cache.vscale"),
                  _operand(c.table, dev, i32, (rows, width), "cache.table"), _operand(c.lengths, dev, i32, (rows,), "cache.lengths"),
                  _operand(c.refs, dev, i32, (pages,), "cache.refs"), pages, rows, width, heads, d, block)
-    have = (desc, ctypes.byref(desc), dev, int(lib.cafeq_cache_pages_workspace_bytes(ctypes.byref(desc))))
+    have = (desc, ctypes.byref(desc), dev, int(lib.cafeq_cache_pages_workspace_bytes(ctypes.byref(desc))), at)
     object.__setattr__(c, "_desc", have)
     return have
 
@@ -927,7 +930,7 @@ class Reserved(NamedTuple):
 
 def _pages_call(cache):
     dev = torch._C._cuda_getDevice()
-    c, ref, _, nbytes = _cache(cache, dev)
+    c, ref, _, nbytes, _ = _cache(cache, dev)
     return dev, c, ref, cache.k.new_empty(max(256, nbytes), dtype=torch.uint8), torch._C._cuda_getCurrentRawStream(dev)
 
 

@@ -47,7 +47,7 @@ AttendPlan plan_few(const cafeq_cache& c, const cafeq_attention& a, int64_t rows
   p.tiles = int((rows + 15) / 16);
   p.keep = int(std::min<int64_t>(16, rows));
   // keys that a tile may reach
-  const int64_t keys = a.window > 0 && a.causal ? std::min(room, a.window + 16 + int64_t(128)) : room;
+  const int64_t keys = a.window > 0 && a.causal ? std::min(room, a.window + int64_t(16 + 128)) : room;
   const int64_t groups = int64_t(c.sequences) * p.tiles * c.heads;
   // Two workgroups a compute unit at once, but none with less than 128 keys (a step a wave) or more than 2048 (lengths differ); half as long where
   // that leaves few to choose from.  us with 128 / 256 / 512 keys: 512 of 4 heads of 256 11.3 / 13.6 / 14.8, 4096 12.0 / 13.7 / 18.2; 32768 of 8 heads with
@@ -55,6 +55,8 @@ AttendPlan plan_few(const cafeq_cache& c, const cafeq_attention& a, int64_t rows
   // 1024 / 2048 60 / 76.
   int64_t part = std::min<int64_t>(2048, std::max<int64_t>(128, keys * groups / 512));
   while (part > 512 && keys * groups / part < 1024) part /= 2;
+  // room that sequences do not use is cut too, into workgroups that end at once: not too many of them
+  while (keys * groups / part > 16384) part *= 2;
   p.span = int((part + 31) / 32);
   p.span = std::max<int>(p.span, int((keys + int64_t(32) * 65535 - 1) / (int64_t(32) * 65535)));      // a grid's second dimension
   p.splits = int((keys + 32 * int64_t(p.span) - 1) / (32 * int64_t(p.span)));
@@ -68,7 +70,7 @@ AttendPlan plan_many(const cafeq_cache& c, const cafeq_attention& a, int64_t few
   p.few_rows = int(few_rows);
   p.units = Units{p.rep, tile, 1};
   p.keep = tile;
-  const int64_t keys = a.window > 0 && a.causal ? std::min(room, a.window + tile / p.rep + int64_t(2 * kt)) : room;
+  const int64_t keys = a.window > 0 && a.causal ? std::min(room, a.window + int64_t(tile / p.rep + 2 * kt)) : room;
   const int64_t groups = p.units.count(a.n, c.sequences) * c.heads;
   // workgroups for what the chip holds at once, none with less than 512 keys
   const int64_t slots = int64_t(device_cu_count()) * many_resident(a.dtype, db) * 4 / many_waves(a.dtype, db);
@@ -82,6 +84,7 @@ AttendPlans plan(const cafeq_cache& c, const cafeq_attention& given) {
   AttendPlans s{};
   cafeq_attention a = given;
   a.longest = std::min(a.longest, a.n);
+  if (a.window >= kMaxKeys) a.window = 0;      // reaches all keys: no position is further from the first
   const int64_t rep = a.heads_q / c.heads, rows = a.longest * rep, room = int64_t(c.width) * c.block;
   const int64_t few = few_rows(c);
   s.many = rows > few;

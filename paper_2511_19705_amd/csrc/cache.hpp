@@ -6,14 +6,14 @@
 namespace cafeq {
 
 constexpr int kCacheDMax = 256;
-constexpr int64_t kMaxSeqs = 65535, kMaxHeads = 4096;
+constexpr int64_t kMaxSeqs = 65535, kMaxHeads = 4096, kMaxKeys = int64_t(1) << 30;
 
 inline int check_cache(const cafeq_cache* c) {
   if (!c || !c->k || !c->v || !c->kscale || !c->vscale || (c->sequences && (!c->table || !c->lengths))) return CAFEQ_ERR_INVALID_ARG;
   if (c->sequences < 0 || c->width < 1 || c->heads < 1 || c->pages < 1 || c->d < 16 || c->d % 16) return CAFEQ_ERR_BAD_SHAPE;
   if (c->block != 16 && c->block != 32 && c->block != 64 && c->block != 128) return CAFEQ_ERR_UNSUPPORTED;
   if (c->d > kCacheDMax || c->heads > kMaxHeads || c->sequences > kMaxSeqs || c->pages > INT32_MAX || c->pages * c->heads > INT32_MAX ||
-      int64_t(c->width) * c->block > INT32_MAX)
+      int64_t(c->width) * c->block > kMaxKeys)
     return CAFEQ_ERR_UNSUPPORTED;
   if (!aligned_to(c->k, 16) || !aligned_to(c->v, 16) || !aligned_to(c->kscale, 4) || !aligned_to(c->vscale, 4) || !aligned_to(c->table, 4) ||
       !aligned_to(c->lengths, 4) || !aligned_to(c->refs, 4))

@@ -346,6 +346,60 @@ def test_captured_graphs_follow_the_lengths(env, counts, lengths, room):
     _near(env, cache, q, _starts(counts), *outs[0])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("window", [2 ** 30 - 1, 2 ** 30, 2 ** 31 - 1])
+def test_the_largest_windows(env, dtype, causal, window):
+    torch, cafeq = env
+    for counts, lengths in (([1, 2], [300, 1]), ([90, 5], [70, 300])):       # rows before the beginning too
+        cache = _cache(env, lengths, 2, 64, 32)
+        starts = torch.tensor(_starts(counts), dtype=torch.int32, device="cuda:0")
+        q = torch.randn((sum(counts), 4, 64), device="cuda:0").to(torch.float32 if dtype == "f32" else torch.bfloat16)
+        want = cafeq.cache_attend(cache, q, starts, causal=causal, lse=True)
+        got = cafeq.cache_attend(cache, q, starts, causal=causal, window=window, lse=True)
+        _near(env, cache, q, _starts(counts), *got, causal=causal)
+        assert torch.equal(torch.isneginf(got[1]), torch.isneginf(want[1]))
+
+
+def test_far_more_room_than_tokens(env):
+    torch, cafeq = env
+    lengths = [700, 3, 64, 5000] * 4
+    for counts in ([1] * 16, [40] * 16):
+        small = _cache(env, [max(n, m) for n, m in zip(lengths, counts)], 2, 64, 64)
+        table = torch.full((16, 1 << 16), -1, dtype=torch.int32, device="cuda:0")
+        table[:, :small.table.shape[1]] = small.table
+        _run(env, counts, lengths, 4, 2, 64, 64, "bf16", cache=small._replace(table=table), window=0)
+        _run(env, counts, lengths, 4, 2, 64, 64, "bf16", cache=small._replace(table=table), window=100)
+
+
+@pytest.mark.parametrize("rep", [128, 300])
+def test_one_key_head_for_many(env, rep):
+    for dtype in ("bf16", "f32"):
+        _run(env, [1, 0, 3], [200, 5, 70], rep, 1, 64, 32, dtype)
+        _run(env, [1], [3000], rep, 1, 128, 64, dtype)
+
+
+def test_a_cache_whose_tensors_are_replaced_or_moved(env):
+    torch, cafeq = env
+    cache, other = (_cache(env, [300, 200], 2, 64, 64, seed=s) for s in (1, 2))
+    q = torch.randn((2, 4, 64), device="cuda:0")
+    s = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda:0")
+    one, two = cafeq.cache_attend(cache, q, s), cafeq.cache_attend(other, q, s)
+    assert not torch.equal(one, two)
+    for name in cache._fields:
+        setattr(cache, name, getattr(other, name).detach())      # (the same memory, a tensor of its own)
+    assert torch.equal(cafeq.cache_attend(cache, q, s), two)
+    cache.k.set_(cache.k.clone())
+    other.k.zero_()
+    assert torch.equal(cafeq.cache_attend(cache, q, s), two)
+    cache.k.set_(cache.k[:, :, :, :32])
+    with pytest.raises(cafeq.CafeqError):
+        cafeq.cache_attend(cache, q, s)
+    cache.k = None
+    with pytest.raises((cafeq.CafeqError, AttributeError)):
+        cafeq.cache_attend(cache, q, s)
+
+
 def test_refusals(env):
     torch, cafeq = env
     cache = _cache(env, [100, 50], 2, 64, 32)
