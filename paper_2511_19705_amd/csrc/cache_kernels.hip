@@ -50,6 +50,8 @@ __device__ __forceinline__ uint4 rescaled(const uint4& w, float ratio, int keep)
 
 // A workgroup stores what a sequence's new tokens bring to one page and head, keys or values.  A thread takes eight channels of four tokens that
 // share a dword of v, reads them once, and writes them as eight codes a token (k) or four a channel (v).  NG: such groups a thread holds.
+// Bound by memory, and for single tokens by five loads one after another (starts, length, page, token, scale).  8192 tokens of 8 heads of 256: 30 us (3.4 TB/s; read
+// twice, with v stored byte by byte, 82); one token each of 64 sequences, 16 heads of 128: 8.2.
 template <class Tag, int T, int NG>
 __global__ __launch_bounds__(T) void append_kernel(const AppendArgs a) {
   using elem = typename Tag::elem;
@@ -198,7 +200,8 @@ __device__ __forceinline__ void page_values(const ValueArgs& a, int side, int he
   }
 }
 
-// A workgroup: what one page and head hold of a sequence's rows, keys or values.
+// A workgroup: what one page and head hold of a sequence's rows, keys or values.  8192 tokens of 8 heads of 256 to bfloat16: 20 us (5.0 TB/s); four heads a
+// workgroup 24.
 template <class Tag>
 __global__ __launch_bounds__(kThreads) void values_kernel(const ValueArgs a) {
   const cafeq_cache& c = a.c;

@@ -1,5 +1,6 @@
 // Pages of the cache: room for new tokens, rows taken over from others, pages moved to the front.  Decided by one workgroup on the
-// device, so that no call waits for the host; what is copied is copied by a second launch over the whole chip.
+// device, so that no call waits for the host; what is copied is copied by a second launch over the whole chip.  Bound by latency where little is copied
+// (32 rows of 33 blocks: reorder 3.0 us, reserve 7.6, 28 copies of 131 KB 4.8) and by memory where much is (1600 pages of 262 KB moved: 159 us, 5.3 TB/s).
 #include "cache.hpp"
 #include "cafeq_internal.hpp"
 

