@@ -915,8 +915,8 @@ def cache_attend(cache, q, starts, longest=None, scale=None, softcap=0.0, window
         pa = ctypes.byref(a)
         nbytes = lib.cafeq_cache_attend_workspace_bytes(ref, pa)
         # the buffer is of this call alone, so that streams share nothing
-        ws = q.new_empty(nbytes, dtype=torch.uint8).data_ptr() if nbytes else None
-        rc = lib.cafeq_cache_attend(ref, pa, ws, stream)
+        ws = q.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+        rc = lib.cafeq_cache_attend(ref, pa, _ptr(ws), stream)      # (held until the launch is made: another thread may allocate)
         if rc:
             _check(rc)
     return (out, sums) if lse else out
