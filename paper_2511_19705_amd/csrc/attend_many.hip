@@ -240,64 +240,39 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
         float f[kRuns];
 #pragma unroll
         for (int k = 0; k < kRuns; ++k) f[k] = unit[t] * ksc[k];
-        float base = 0.f;      // x f + base: the score in log2
         if (a.softcap > 0.f) {
           const float in = kF32 ? 1.f / a.softcap : 2.f * kLog2e * __builtin_amdgcn_rcpf(a.softcap), out = a.softcap * kLog2e;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float z = x[t][e] * (f[e / kRun] * in);
-            // out tanh(z) = out - 2 out / (1 + e^2z): the fraction here, the rest where the exponent is formed
-            if constexpr (kF32) x[t][e] = capped<true>(z, out);
-            else x[t][e] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(z));
-          }
+          for (int e = 0; e < 16; ++e) x[t][e] = capped<kF32>(x[t][e] * (f[e / kRun] * in), out);
 #pragma unroll
-          for (int k = 0; k < kRuns; ++k) f[k] = kF32 ? 1.f : 2.f * out;
-          base = kF32 ? 0.f : out;
+          for (int k = 0; k < kRuns; ++k) f[k] = 1.f;
         }
-        float top = kNoKey, ex[kRuns], mant[kRuns];
-#pragma unroll
-        for (int k = 0; k < kRuns; ++k) {
-          ex[k] = sc[k].exp + base;
-          mant[k] = sc[k].mant;
-        }
+        float top = kNoKey;
+        const int from = klo[t] - key0 - 4 * h, to = khi[t] - key0 - 4 * h;
+        auto in = [&](int e) { return bool(int(8 * (e >> 2) + (e & 3) >= from) & int(8 * (e >> 2) + (e & 3) < to) & int(!gone[e / kRun])); };
         if (!odd) {
 #pragma unroll
           for (int k = 0; k < kRuns; ++k) {
             float y = x[t][kRun * k];
 #pragma unroll
             for (int e = 1; e < kRun; ++e) y = fmaxf(y, x[t][kRun * k + e]);
-            top = fmaxf(top, fmaf(y, f[k], ex[k]));
+            top = fmaxf(top, fmaf(y, f[k], sc[k].exp));
           }
         } else {
-          // Scores here, -inf for keys that do not count.  A run without any takes nothing from its page, whose scale may be no number.
-          const int from = klo[t] - key0 - 4 * h, to = khi[t] - key0 - 4 * h;
 #pragma unroll
           for (int k = 0; k < kRuns; ++k) {
-            float y = -INFINITY;
+            float y = kNoKey;
 #pragma unroll
-            for (int e = kRun * k; e < kRun * k + kRun; ++e) {
-              const int at = 8 * (e >> 2) + (e & 3);
-              x[t][e] = int(at >= from) & int(at < to) & int(!gone[k]) ? fmaf(x[t][e], f[k], base) : -INFINITY;
-              y = fmaxf(y, x[t][e]);
-            }
-            f[k] = 1.f;
-            ex[k] = sc[k].exp;
-            bool any = false;
-#pragma unroll
-            for (int e = kRun * k; e < kRun * k + kRun; e += 4) any |= max(from, 2 * e) < min(to, 2 * e + 4);
-            any &= !gone[k];
+            for (int e = kRun * k; e < kRun * k + kRun; ++e) y = in(e) ? fmaxf(y, x[t][e] * f[k]) : y;
             if (sc[k].zero) {
               // keys of a page of zeros count in the sum of weights only, on a maximum of their own
               const float most = fmaxf(mz[t], other_half(y));
               lz[t] *= __builtin_amdgcn_exp2f(mz[t] - most);
               mz[t] = most;
 #pragma unroll
-              for (int e = kRun * k; e < kRun * k + kRun; ++e) lz[t] += __builtin_amdgcn_exp2f(x[t][e] - most);
-              ex[k] = -INFINITY;
+              for (int e = kRun * k; e < kRun * k + kRun; ++e) lz[t] += in(e) ? __builtin_amdgcn_exp2f(x[t][e] * f[k] - most) : 0.f;
             } else {
-              top = any ? fmaxf(top, y + ex[k]) : top;
-              ex[k] = any ? ex[k] : 0.f;
-              mant[k] = any ? mant[k] : 1.f;
+              top = y == kNoKey ? top : fmaxf(top, y + sc[k].exp);
             }
           }
         }
@@ -312,13 +287,23 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
         float P[16];
 #pragma unroll
         for (int k = 0; k < kRuns; ++k) {
-          const float shift = ex[k] - M[t];
+          const float shift = sc[k].exp - M[t];
           float sum = 0.f;
 #pragma unroll
-          for (int e = kRun * k; e < kRun * k + kRun; ++e) {
-            P[e] = __builtin_amdgcn_exp2f(fmaf(x[t][e], f[k], shift));
-            sum += P[e];
-            if constexpr (kF32) P[e] *= mant[k];
+          for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] = __builtin_amdgcn_exp2f(fmaf(x[t][e], f[k], shift));
+          if (odd) {      // a scale that is no number must not reach keys that do not count
+#pragma unroll
+            for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] = int(in(e)) & int(!sc[k].zero) ? P[e] : 0.f;
+          }
+#pragma unroll
+          for (int e = kRun * k; e < kRun * k + kRun; ++e) sum += P[e];
+          if constexpr (kF32) {
+#pragma unroll
+            for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] *= sc[k].mant;
+            if (odd) {
+#pragma unroll
+              for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] = int(in(e)) & int(!sc[k].zero) ? P[e] : 0.f;
+            }
           }
           l[t] = sum == 0.f ? l[t] : fmaf(sum, sc[k].inv, l[t]);      // (nothing times a scale that is no number is nothing)
         }
