@@ -347,7 +347,8 @@ int cafeq_cache_values(const cafeq_cache* cache, const int32_t* begin, const int
  *   out = sum_t exp(x_t) V_t / sum_t exp(x_t),  lse = log sum_t exp(x_t)   (a row without keys: 0 and -inf)
  * K, V: the codes times their scales, which are not negative.  q, out float32 or bfloat16 (dtype); lse float32 [n][heads_q] dense or NULL.  Queries of bfloat16 are
  * taken exactly (magnitudes below 2^-28 of the row's largest to multiples of 2^-39 of it), probabilities rounded to 11 bits (below 2^-28 of the
- * largest, weighed with the scale of v, to multiples of 2^-39 of it); with float32 both are taken in two such parts.  Sums are float32 in a fixed order.  A row of q that holds a NaN or an infinity gives NaN.  A page and head of v with a scale below 2^-100 counts as zeros.
+ * largest, weighed with the scale of v, to multiples of 2^-39 of it); with float32 both are taken in two such parts.  Sums are float32 in a fixed order.  A row of q that holds a NaN or an infinity gives NaN.  A page and head of v with a scale below 2^-100 counts as zeros;
+ * where scales of a head lie more than 2^100 apart the weight of the smaller ones' keys may be lost.
  * Rows start at multiples of 16 bytes; out overlaps no input.  longest as in cafeq_cache_append (rows beyond it are left).
  * heads_q a multiple of heads, up to 4096; n up to 2^24, n * heads_q below 2^31.  ws: cafeq_cache_attend_workspace_bytes() bytes (may be 0), 16-byte aligned. */
 typedef struct {
