@@ -345,6 +345,7 @@ int cafeq_cache_values(const cafeq_cache* cache, const int32_t* begin, const int
  * head h reads key head h / (heads_q / heads):
  *   x_t = scale q . K_t, with softcap > 0: softcap tanh(x_t / softcap);  keys t: 0 <= t < lengths[i], t <= p if causal, t > p - window if window > 0
  *   out = sum_t exp(x_t) V_t / sum_t exp(x_t),  lse = log sum_t exp(x_t)   (a row without keys: 0 and -inf)
+ * Scores are float32 numbers of any magnitude up to 2^126 (a row whose largest passes 2^126 is not specified); from 2^12 on a row may take them against a whole number near its largest.
  * K, V: the codes times their scales, which are not negative.  q, out float32 or bfloat16 (dtype); lse float32 [n][heads_q] dense or NULL.  Queries of bfloat16 are
  * taken exactly (magnitudes below 2^-28 of the row's largest to multiples of 2^-39 of it), probabilities rounded to 11 bits (below 2^-28 of the
  * largest, weighed with the scale of v, to multiples of 2^-39 of it); with float32 both are taken in two such parts.  Sums are float32 in a fixed order.  A row of q that holds a NaN or an infinity gives NaN.  A page and head of v with a scale below 2^-100 counts as zeros;

@@ -18,7 +18,7 @@ using half8_t = __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16;
 using f32x4_t = __attribute__((__vector_size__(4 * sizeof(float)))) float;
 using f32x16_t = __attribute__((__vector_size__(16 * sizeof(float)))) float;
 
-constexpr float kNoKey = -1.7e38f;       // M before the first key
+constexpr float kNoKey = -FLT_MAX;       // M before the first key
 constexpr float kTop = 14.f;              // log2 of the largest p
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kZeroScale = 0x1p-100f;  // pages of v below it hold zeros: their keys have weight, and no value
@@ -84,6 +84,25 @@ __device__ __forceinline__ ValueScale value_scale(float vs) {
   s.mant = plain ? __uint_as_float((u & 0x7FFFFFu) | 0x3F800000u) : s.zero ? 0.f : vs;
   s.inv = plain ? __uint_as_float((254u - e) << 23) : 1.f;
   return s;
+}
+
+// Large scores.  The weight's argument is one fused operation, x f - M, while M comes of rounded scores x f: where half a step of the score is one and more the two
+// do not fit together (and exp - M is rounded where exp is no whole number).  So where a step of keys may hold scores beyond kFar, a row whose largest one passes kLarge
+// takes them against a reference of its own, a whole number that follows the largest one: x' = fl(x f) - base is exact where it counts, and M, o and l go on as they
+// are, in units of 2^(base + M).  Rows that meet no such score keep their bits, whatever the rows beside them hold.
+constexpr float kFar = 0x1p19f, kLarge = 0x1p12f;
+// x f is below kFar for all keys where f is below this: |q| < 2^15, |code| <= 2^7, 64 db channels
+constexpr float near_factor(int db) { return kFar / (64.f * db * 0x1p22f); }
+// the reference that a row goes on with (0: none), top being its largest score of these keys (kNoKey: none)
+__device__ __forceinline__ float next_base(float top, float base, bool first) {
+  const bool leaves = base != 0.f ? top > base : fabsf(top) > kLarge && (top > 0.f || first);
+  return leaves && top > kNoKey ? ceilf(top) : base;
+}
+// What a wave's o and l are times in the end, and the M that they are then in units of: a float32 of its own again, base + M, however far it is
+struct Finish { float all, unit; };
+__device__ __forceinline__ Finish finish_of(float M, float base) {
+  const float all = base + M;
+  return {all, __builtin_amdgcn_exp2f(M - (all - base))};
 }
 
 // Rows of q are taken times a power of two that brings the largest magnitude (its bits) to [2^14, 2^15): bfloat16 then is exact in float16 down to

@@ -45,7 +45,8 @@ __global__ __launch_bounds__(kThreads, Tag::dtype == CAFEQ_F32 && DB == 4 ? 1 : 
   half8_t* q_lds = reinterpret_cast<half8_t*>(lds);      // [part][64 channels][8 of 16][lane]: the rows as the first product takes them
   float* unit_lds = lds + kParts * DB * 2 * 64 * 4;      // [16]
   float* sum_lds = unit_lds + kTile;                     // [kWaves][16][2]
-  float* out_lds = sum_lds + kWaves * kTile * 2;          // [kWaves][keep][d + 4]
+  float* base_lds = sum_lds + kWaves * kTile * 2;         // [kWaves][16]: references of rows whose scores are large
+  float* out_lds = base_lds + kWaves * kTile;             // [kWaves][keep][d + 4]
   const int krun = 16 * ((l16 >> 2) & 1), vrun = 16 * (g & 1), mine = vrun + 8 * (g >> 1);
   const int32_t* table = c.table + int64_t(i) * c.width;
   // without a window the first step is known before the lengths are: its pages are on their way with them
@@ -150,6 +151,7 @@ __global__ __launch_bounds__(kThreads, Tag::dtype == CAFEQ_F32 && DB == 4 ? 1 : 
 #pragma unroll
   for (int m = 0; m < 2 * kPairs; ++m) o[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   float M = kNoKey, l = 0.f, mz = kNoKey, lz = 0.f;      // mz, lz: keys whose page of v is zeros
+  bool based = false;                                    // whether a row of the wave has a reference
 
   for (; step < end; step += kWaves * NS) {
     const int key0 = step * kStep, next = step + kWaves * NS;
@@ -205,8 +207,12 @@ __global__ __launch_bounds__(kThreads, Tag::dtype == CAFEQ_F32 && DB == 4 ? 1 : 
       }
     }
     if (next < end) load_k(next);
+    bool far = false;      // whether scores may be large
+#pragma unroll
+    for (int n = 0; n < NS; ++n) far |= f[n] > near_factor(DB);
     if (a.softcap > 0.f) {
       const float in = kF32 ? 1.f / a.softcap : 2.f * kLog2e * __builtin_amdgcn_rcpf(a.softcap), out = a.softcap * kLog2e;
+      far &= out > kFar;
 #pragma unroll
       for (int n = 0; n < NS; ++n) {
 #pragma unroll
@@ -215,6 +221,8 @@ __global__ __launch_bounds__(kThreads, Tag::dtype == CAFEQ_F32 && DB == 4 ? 1 : 
       }
     }
     auto in = [&](int n, int e) { return bool(int(e >= from[n]) & int(e < to[n]) & int(!s[n].zero)); };
+    far = __ballot(far) != 0;
+    odd |= based || far;
     float top = kNoKey;
     if (!odd) {
 #pragma unroll
@@ -225,6 +233,25 @@ __global__ __launch_bounds__(kThreads, Tag::dtype == CAFEQ_F32 && DB == 4 ? 1 : 
         top = fmaxf(top, t + s[n].exp);
       }
     } else {
+      if (based || far) {
+        float most = kNoKey;
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) most = in(n, e) ? fmaxf(most, x[n][e >> 2][e & 3] * f[n]) : most;
+        const float old = based ? base_lds[wave * kTile + l16] : 0.f, base = next_base(across(most), old, M == kNoKey);
+        M = M == kNoKey ? M : M + (old - base);
+        based = __ballot(base != 0.f) != 0;
+        if (based) base_lds[wave * kTile + l16] = base;
+        if (base != 0.f) {
+#pragma unroll
+          for (int n = 0; n < NS; ++n) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[n][e >> 2][e & 3] = x[n][e >> 2][e & 3] * f[n] - (s[n].zero ? 0.f : base);
+            f[n] = 1.f;
+          }
+        }
+      }
 #pragma unroll
       for (int n = 0; n < NS; ++n) {
         float t = kNoKey;
@@ -301,14 +328,15 @@ __global__ __launch_bounds__(kThreads, Tag::dtype == CAFEQ_F32 && DB == 4 ? 1 : 
   // the wave's sums, then the waves'
   l = sum_across(l);
   lz = sum_across(lz);
-  const float both = fmaxf(M, mz), own = __builtin_amdgcn_exp2f(M - both);
-  l = l * own + lz * __builtin_amdgcn_exp2f(mz - both);
+  const Finish fin = finish_of(M, based ? base_lds[wave * kTile + l16] : 0.f);
+  const float both = fmaxf(fin.all, mz);
+  l = l * (fin.unit * __builtin_amdgcn_exp2f(fin.all - both)) + lz * __builtin_amdgcn_exp2f(mz - both);
   if (g == 0) *reinterpret_cast<float2*>(sum_lds + 2 * (wave * kTile + l16)) = make_float2(both, l);
   __syncthreads();
   float top = kNoKey;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sum_lds[2 * (w * kTile + l16)]);
-  const float mul = __builtin_amdgcn_exp2f(M - top);
+  const float mul = fin.unit * __builtin_amdgcn_exp2f(fin.all - top);
   if (l16 < p.keep) {
     float* at = out_lds + (wave * p.keep + l16) * ld + 4 * g;
 #pragma unroll
@@ -388,7 +416,7 @@ int launch(const AttendPlan& p, hipStream_t st) {
   // 48 sequences of 1600 to 32700 keys, 16 heads of 128, sequences innermost: 842 us, heads innermost 629.
   const dim3 grid(unsigned(p.c.heads * p.tiles), unsigned(p.splits), unsigned(p.c.sequences));
   const int parts = Tag::dtype == CAFEQ_F32 ? 2 : 1;
-  const size_t lds = sizeof(float) * (parts * DB * 2 * 64 * 4 + kTile + kWaves * kTile * 2 + size_t(kWaves) * p.keep * (p.c.d + 4));
+  const size_t lds = sizeof(float) * (parts * DB * 2 * 64 * 4 + kTile + kWaves * kTile * 3 + size_t(kWaves) * p.keep * (p.c.d + 4));
   const auto kern = attend_few_kernel<Tag, DB, EXACT>;
   if (lds > 65536) {
     static const bool ok = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess;

@@ -7,6 +7,10 @@ namespace {
 
 constexpr int kJoin = 256;
 
+// What of a lane's row is rarely looked at, in LDS, [what][thread]: the registers serve the tiles.  Keys in its reach; its reference where scores are large;
+// the maximum and the sum of keys on pages of zeros
+enum RowPart { kFirstKey, kEndKey, kBase, kZeroMax, kZeroSum, kRowParts };
+
 __device__ __forceinline__ float other_half(float v) {
   const uint32_t u = __float_as_uint(v);
   const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
@@ -176,11 +180,29 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
   };
 
   f32x16_t o[QT][MT];
-  float M[QT], l[QT], mz[QT], lz[QT];
+  float M[QT], l[QT];
+  float* row_lds = reinterpret_cast<float*>(buf + 2 * kBuf) + tid;
+  auto row = [&](int t, int what) -> float& { return row_lds[(what * QT + t) * kThreads]; };
+  // scales of k (their bits) from which on scores of the wave's rows may be large; 0 once a row has a reference
+  float most_unit = 0.f;
+#pragma unroll
+  for (int t = 0; t < QT; ++t) most_unit = fmaxf(most_unit, unit[t]);
+#pragma unroll
+  for (int k = 1; k < 32; k <<= 1) most_unit = fmaxf(most_unit, __shfl_xor(most_unit, k));
+  const bool bounded = a.softcap > 0.f && a.softcap * kLog2e <= kFar;
+  const uint32_t near_scale = __builtin_amdgcn_readfirstlane(bounded ? 0xFFFFFFFFu : max(1u, __float_as_uint(near_factor(DB) / most_unit)));
+  uint32_t far_scale = near_scale;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    M[t] = mz[t] = kNoKey;
-    l[t] = lz[t] = 0.f;
+    row(t, kFirstKey) = __int_as_float(klo[t]);
+    row(t, kEndKey) = __int_as_float(khi[t]);
+    row(t, kZeroMax) = kNoKey;
+    row(t, kZeroSum) = 0.f;
+  }
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    M[t] = kNoKey;
+    l[t] = 0.f;
 #pragma unroll
     for (int m = 0; m < MT; ++m) o[t][m] = f32x16_t{};
   }
@@ -220,14 +242,15 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
       constexpr int kRuns = ONE ? 1 : 2, kRun = 16 / kRuns;
       ValueScale sc[kRuns];
       float ksc[kRuns];
-      bool gone[kRuns], odd = key0 < all_lo || key0 + 32 > all_hi;
+      bool gone[kRuns], far = false, odd = key0 < all_lo || key0 + 32 > all_hi;
 #pragma unroll
       for (int k = 0; k < kRuns; ++k) {
         const int at = ONE ? 0 : 2 * n + k;
         ksc[k] = lane_value(tks, at);
         sc[k] = value_scale(lane_value(tvs, at));
         gone[k] = __builtin_amdgcn_readlane(int(thole), at);
-        odd |= gone[k] || sc[k].zero || !(ksc[k] >= 0.f);
+        far |= __float_as_uint(ksc[k]) >= far_scale;
+        odd |= gone[k] || sc[k].zero || !(ksc[k] >= 0.f) || far;
         if constexpr (!kF32) {
           // the mantissa goes into the exponent too: one rounding of the argument for the page, for a multiplication a weight
           sc[k].exp += __builtin_amdgcn_logf(sc[k].mant);
@@ -248,9 +271,13 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
           for (int k = 0; k < kRuns; ++k) f[k] = 1.f;
         }
         float top = kNoKey;
-        const int from = klo[t] - key0 - 4 * h, to = khi[t] - key0 - 4 * h;
+        int from = 0, to = 0;
+        if (__builtin_expect(odd, 0)) {
+          from = __float_as_int(row(t, kFirstKey)) - key0 - 4 * h;
+          to = __float_as_int(row(t, kEndKey)) - key0 - 4 * h;
+        }
         auto in = [&](int e) { return bool(int(8 * (e >> 2) + (e & 3) >= from) & int(8 * (e >> 2) + (e & 3) < to) & int(!gone[e / kRun])); };
-        if (!odd) {
+        if (__builtin_expect(!odd, 1)) {
 #pragma unroll
           for (int k = 0; k < kRuns; ++k) {
             float y = x[t][kRun * k];
@@ -259,20 +286,38 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
             top = fmaxf(top, fmaf(y, f[k], sc[k].exp));
           }
         } else {
+          if (__builtin_expect(far, 0)) {
+            float high = kNoKey;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) high = int(in(e)) & int(!sc[e / kRun].zero) ? fmaxf(high, x[t][e] * f[e / kRun]) : high;
+            const float old = far_scale == 0u ? row(t, kBase) : 0.f, base = next_base(other_half(high), old, M[t] == kNoKey);
+            M[t] = M[t] == kNoKey ? M[t] : M[t] + (old - base);
+            far_scale = __ballot(base != 0.f) ? 0u : near_scale;
+            if (far_scale == 0u) row(t, kBase) = base;
+            if (base != 0.f) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) x[t][e] = x[t][e] * f[e / kRun] - (sc[e / kRun].zero ? 0.f : base);
+#pragma unroll
+              for (int k = 0; k < kRuns; ++k) f[k] = 1.f;
+            }
+          }
 #pragma unroll
           for (int k = 0; k < kRuns; ++k) {
             float y = kNoKey;
 #pragma unroll
-            for (int e = kRun * k; e < kRun * k + kRun; ++e) y = in(e) ? fmaxf(y, x[t][e] * f[k]) : y;
+            for (int e = kRun * k; e < kRun * k + kRun; ++e) y = in(e) ? fmaxf(y, x[t][e]) : y;
             if (sc[k].zero) {
               // keys of a page of zeros count in the sum of weights only, on a maximum of their own
-              const float most = fmaxf(mz[t], other_half(y));
-              lz[t] *= __builtin_amdgcn_exp2f(mz[t] - most);
-              mz[t] = most;
+              float mz = row(t, kZeroMax), lz = row(t, kZeroSum);
+              const float most = fmaxf(mz, other_half(y == kNoKey ? y : y * f[k]));
+              lz *= __builtin_amdgcn_exp2f(mz - most);
+              mz = most;
 #pragma unroll
-              for (int e = kRun * k; e < kRun * k + kRun; ++e) lz[t] += in(e) ? __builtin_amdgcn_exp2f(x[t][e] * f[k] - most) : 0.f;
+              for (int e = kRun * k; e < kRun * k + kRun; ++e) lz += in(e) ? __builtin_amdgcn_exp2f(x[t][e] * f[k] - most) : 0.f;
+              row(t, kZeroMax) = mz;
+              row(t, kZeroSum) = lz;
             } else {
-              top = y == kNoKey ? top : fmaxf(top, y + sc[k].exp);
+              top = y == kNoKey ? top : fmaxf(top, fmaf(y, f[k], sc[k].exp));
             }
           }
         }
@@ -291,7 +336,7 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
           float sum = 0.f;
 #pragma unroll
           for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] = __builtin_amdgcn_exp2f(fmaf(x[t][e], f[k], shift));
-          if (odd) {      // a scale that is no number must not reach keys that do not count
+          if (__builtin_expect(odd, 0)) {      // a scale that is no number must not reach keys that do not count
 #pragma unroll
             for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] = int(in(e)) & int(!sc[k].zero) ? P[e] : 0.f;
           }
@@ -300,7 +345,7 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
           if constexpr (kF32) {
 #pragma unroll
             for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] *= sc[k].mant;
-            if (odd) {
+            if (__builtin_expect(odd, 0)) {
 #pragma unroll
               for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] = int(in(e)) & int(!sc[k].zero) ? P[e] : 0.f;
             }
@@ -338,10 +383,11 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
   const int64_t part = ((w * c.heads + head) * p.splits + split) * kTile;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    const int row = wave * 32 * QT + 32 * t + l32, R = first + row;
-    float sum = l[t] + __shfl_xor(l[t], 32), sumz = lz[t] + __shfl_xor(lz[t], 32);
-    const float both = fmaxf(M[t], mz[t]), own = __builtin_amdgcn_exp2f(M[t] - both);
-    const float total = sum * own + sumz * __builtin_amdgcn_exp2f(mz[t] - both);
+    const int place = wave * 32 * QT + 32 * t + l32, R = first + place;
+    float sum = l[t] + __shfl_xor(l[t], 32), lz = row(t, kZeroSum), sumz = lz + __shfl_xor(lz, 32), mz = row(t, kZeroMax);
+    const Finish fin = finish_of(M[t], far_scale == 0u ? row(t, kBase) : 0.f);
+    const float both = fmaxf(fin.all, mz), own = fin.unit * __builtin_amdgcn_exp2f(fin.all - both);
+    const float total = sum * own + sumz * __builtin_amdgcn_exp2f(mz - both);
     if (R >= r.rows) continue;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -350,10 +396,10 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
         const int ch = 32 * m + 2 * e + 4 * h;
         if (!EXACT && ch >= d) continue;
         const f32x4_t v = f32x4_t{o[t][m][e], o[t][m][e + 1], o[t][m][e + 2], o[t][m][e + 3]} * own;
-        if (used > 1) *reinterpret_cast<f32x4_t*>(p.parts + (part + row) * d + ch) = v;
+        if (used > 1) *reinterpret_cast<f32x4_t*>(p.parts + (part + place) * d + ch) = v;
         else store_row<Tag>(p, r, R, head, ch, v, both, total);
       }
-    if (used > 1 && h == 0) *reinterpret_cast<float2*>(p.sums + 2 * (part + row)) = make_float2(both, total);
+    if (used > 1 && h == 0) *reinterpret_cast<float2*>(p.sums + 2 * (part + place)) = make_float2(both, total);
   }
 }
 
@@ -390,7 +436,7 @@ __global__ __launch_bounds__(kJoin) void attend_many_join_kernel(const AttendPla
 template <class Tag, int DB, bool EXACT, bool ONE>
 int launch_one(const AttendPlan& p, hipStream_t st) {
   constexpr int KT = many_keys(Tag::dtype, DB), kWaves = many_waves(Tag::dtype, DB), kTile = 32 * kWaves;
-  constexpr size_t lds = 2 * 16 * (2 * 4 * DB * (KT + 1) + 2 * (KT / 16) * (64 * DB + 1));
+  constexpr size_t lds = 2 * 16 * (2 * 4 * DB * (KT + 1) + 2 * (KT / 16) * (64 * DB + 1)) + sizeof(float) * kRowParts * 64 * kWaves;
   const auto kern = attend_many_kernel<Tag, DB, EXACT, ONE>;
   if (lds > 65536) {
     static const bool ok = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds)) == hipSuccess;
