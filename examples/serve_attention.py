@@ -45,7 +45,7 @@ class Layer:
         self.cache = cafeq.kv_cache(rows, rows * width, heads, head, block=block, width=width, device=DEVICE)
 
     def step(self, x, starts, longest):
-        """New tokens x [n][d] of the rows that starts gives; their result [n][d]."""
+        """New tokens x [n][d] of the rows that starts gives; their result [n][d].  Without room for them (cache.missing, on the device) the cache stays as it is."""
         n, (hq, h, hd) = x.shape[0], (self.heads_q, self.heads, self.head)
         a = cafeq.norm_quantize(x, self.gain, gain_offset=1.0, group=GROUP)
         y = cafeq.infer_packed(a.codes, self.qkv, xscales=a.scales, xgroup=GROUP, dtype=torch.bfloat16)

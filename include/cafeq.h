@@ -308,7 +308,9 @@ int cafeq_rotate_heads(const cafeq_rotation* cfg, const cafeq_heads* q, const ca
  *   k [pages][heads][block][d]   kscale [pages][heads]        v [pages][heads][d][block]   vscale [pages][heads]
  * (a channel's tokens of v side by side: the order in which the matrix instructions contract over tokens).  table
  * [sequences][width]: the page of each block of a sequence (blocks behind its length: -1); lengths [sequences]: its tokens;
- * refs [pages]: rows of the table that hold a page (0: free; used by reserve, reorder and compact only).  All device memory, owned by the
+ * refs [pages]: rows of the table that hold a page (0: free; used by reserve, reorder and compact only).  missing: what the last
+ * cafeq_cache_reserve lacked, which alone writes it (0 at first).  While it is not 0 append stores nothing, and attend takes no token as a key
+ * (rows are 0, lse -inf): steps that find no room, in a captured graph too, leave the cache as it is.  With NULL the caller sees to that.  All device memory, owned by the
  * caller; k and v 16-byte aligned.  d a multiple of 16 up to 256, block 16, 32, 64 or 128, pages * heads up to 2^31 - 1, heads up to 4096,
  * width * block up to 2^30, sequences up to 65535.  Numbers in device memory are not trusted with addresses: lengths beyond width * block count as
  * that, and tokens whose page is outside [0, pages) are not read or written and are no keys. */
@@ -322,6 +324,7 @@ typedef struct {
   int32_t* refs;
   int64_t pages;
   int32_t sequences, width, heads, d, block;
+  int32_t* missing;       /* [1] or NULL */
 } cafeq_cache;
 
 /* New keys and values k, v [n][heads][d] (float32 or bfloat16) into the pages of their sequences, at the last starts[i+1] - starts[i]
@@ -369,7 +372,7 @@ int cafeq_cache_attend(const cafeq_cache* cache, const cafeq_attention* a, void*
  * reserve: room for starts[i+1] - starts[i] more tokens of each sequence.  Row by row the lowest free pages (refs 0) are taken: first, where the
  *   sequence's last page is partly filled and refs of it exceed 1, one that the page is copied to and that takes its place, then
  *   one for each new block.  lengths grow, refs follow.  positions (int32 [n] or NULL): the position of every new token.  missing
- *   (int32 [1]): 0, or how many pages or table columns lack; then nothing is changed.
+ *   (int32 [1], and the cache's): 0, or how many pages or table columns lack; then nothing is changed, and positions are 0.
  * reorder: row i takes over what row sources[i] held before the call (sources int32 [sequences], any value outside [0, sequences): nothing; the row's own number: it
  *   stays).  The same source may be given several times: pages are shared, refs count their rows.  Pages that no row holds any more are free.
  * compact: pages in use move to the lowest numbers (page by page in order, only those that have to), tables and refs with them; used (int32 [1]): how many there are. */

@@ -87,7 +87,7 @@ class Rotation(ctypes.Structure):
 class Cache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("kscale", ctypes.c_void_p), ("vscale", ctypes.c_void_p), ("table", ctypes.c_void_p),
                 ("lengths", ctypes.c_void_p), ("refs", ctypes.c_void_p), ("pages", ctypes.c_int64), ("sequences", ctypes.c_int32), ("width", ctypes.c_int32),
-                ("heads", ctypes.c_int32), ("d", ctypes.c_int32), ("block", ctypes.c_int32)]
+                ("heads", ctypes.c_int32), ("d", ctypes.c_int32), ("block", ctypes.c_int32), ("missing", ctypes.c_void_p)]
 
 
 class Attention(ctypes.Structure):
@@ -800,12 +800,13 @@ def rotate_heads(q, k, positions, freq, interleaved=False, norm=False, gain_q=No
 
 class KVCache:
     """A cache as cafeq.h describes it: codes and scales of keys and values, the page of each block of a sequence, tokens of a sequence, rows that
-    hold a page.  Its tensors are checked at the first call and after one of them was replaced or moved; their contents may change at will."""
-    __slots__ = ("k", "v", "kscale", "vscale", "table", "lengths", "refs", "_desc")
-    _fields = __slots__[:7]
+    hold a page, what the last cache_reserve lacked (int32 [1], made if not given).  Its tensors are checked at the first call and after one of them was replaced or moved; their contents may change at will."""
+    __slots__ = ("k", "v", "kscale", "vscale", "table", "lengths", "refs", "missing", "_desc")
+    _fields = __slots__[:8]
 
-    def __init__(self, k, v, kscale, vscale, table, lengths, refs):
+    def __init__(self, k, v, kscale, vscale, table, lengths, refs, missing=None):
         self.k, self.v, self.kscale, self.vscale, self.table, self.lengths, self.refs = k, v, kscale, vscale, table, lengths, refs
+        self.missing = torch.zeros(1, dtype=torch.int32, device=refs.device) if missing is None else missing
 
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
@@ -830,11 +831,11 @@ def kv_cache(sequences, pages, heads, d, block=64, width=None, device=None):
 
 
 def _cache(c, dev):
-    """(descriptor, its reference for a call, device, scratch of the page calls, addresses) of a KVCache on device number `dev`.  The checks of seven
+    """(descriptor, its reference for a call, device, scratch of the page calls, addresses) of a KVCache on device number `dev`.  The checks of eight
     tensors (8 us) are made once, and again where one has another address, or k or the table another shape."""
     have = c._desc
-    at = (c.k.data_ptr(), c.v.data_ptr(), c.kscale.data_ptr(), c.vscale.data_ptr(), c.table.data_ptr(), c.lengths.data_ptr(), c.refs.data_ptr(), c.k.shape,
-          c.table.shape)
+    at = (c.k.data_ptr(), c.v.data_ptr(), c.kscale.data_ptr(), c.vscale.data_ptr(), c.table.data_ptr(), c.lengths.data_ptr(), c.refs.data_ptr(),
+          c.missing.data_ptr(), c.k.shape, c.table.shape)
     if have is not None and have[2] == dev and have[4] == at:
         return have
     if len(c.k.shape) != 4 or len(c.table.shape) != 2:
@@ -845,7 +846,7 @@ def _cache(c, dev):
     desc = Cache(_operand(c.k, dev, i8, (pages, heads, block, d), "cache.k"), _operand(c.v, dev, i8, (pages, heads, d, block), "cache.v"),
                  _operand(c.kscale, dev, f32, (pages, heads), "cache.kscale"), _operand(c.vscale, dev, f32, (pages, heads), "cache.vscale"),
                  _operand(c.table, dev, i32, (rows, width), "cache.table"), _operand(c.lengths, dev, i32, (rows,), "cache.lengths"),
-                 _operand(c.refs, dev, i32, (pages,), "cache.refs"), pages, rows, width, heads, d, block)
+                 _operand(c.refs, dev, i32, (pages,), "cache.refs"), pages, rows, width, heads, d, block, _operand(c.missing, dev, i32, (1,), "cache.missing"))
     have = (desc, ctypes.byref(desc), dev, int(lib.cafeq_cache_pages_workspace_bytes(ctypes.byref(desc))), at)
     object.__setattr__(c, "_desc", have)
     return have
@@ -857,7 +858,8 @@ def _starts(t, rows, dev, what="starts"):
 
 def cache_append(cache, k, v, starts, longest=None):
     """cafeq_cache_append: new keys and values [n][heads][d] into the pages of their sequences, in 8 bits.  starts int32 [sequences + 1]: the rows
-    of each sequence, the last of its lengths' tokens; longest: an upper bound of a sequence's rows (n, if not given)."""
+    of each sequence, the last of its lengths' tokens; longest: an upper bound of a sequence's rows (n, if not given).  Behind a cache_reserve
+    that found no room nothing is stored."""
     dev, kind = torch._C._cuda_getDevice(), _FLOATS.get(k.dtype)
     if kind is None or v.dtype is not k.dtype:
         raise CafeqError("k and v must be float32 or bfloat16, both the same")
@@ -891,7 +893,8 @@ def cache_values(cache, begin, starts, n, dtype=torch.float32):
 
 def cache_attend(cache, q, starts, longest=None, scale=None, softcap=0.0, window=0, causal=True, lse=False, out=None):
     """cafeq_cache_attend: attention of new tokens q [n][heads_q][d] over the cache, which holds their keys and values already.  scale: d^-1/2 if
-    not given; softcap, window: 0 for none; starts, longest as in cache_append.  Returns out, or (out, lse [n][heads_q]) with lse=True."""
+    not given; softcap, window: 0 for none; starts, longest as in cache_append.  Returns out, or (out, lse [n][heads_q]) with lse=True.  Behind a
+    cache_reserve that found no room out is 0, lse -inf."""
     dev, kind = torch._C._cuda_getDevice(), _FLOATS.get(q.dtype)
     if kind is None:
         raise CafeqError("q must be float32 or bfloat16")
@@ -936,7 +939,8 @@ def _pages_call(cache):
 
 def cache_reserve(cache, starts, n):
     """cafeq_cache_reserve: room for starts[i + 1] - starts[i] more tokens of each sequence, n in all.  Nothing waits: a caller that cannot be
-    sure of room reads `missing` (one int32 on the device); where it is not 0 nothing has changed and positions hold nothing."""
+    sure of room reads `missing` (one int32 on the device); where it is not 0 nothing has changed, positions are 0, and until a reserve finds room
+    cache_append stores nothing and cache_attend returns zeros."""
     dev, c, ref, ws, stream = _pages_call(cache)
     positions, missing = cache.refs.new_empty(n), cache.refs.new_empty(1)
     _check(lib.cafeq_cache_reserve(ref, _starts(starts, c.sequences, dev), n, positions.data_ptr() if n else None, missing.data_ptr(), ws.data_ptr(), stream))

@@ -64,7 +64,7 @@ __device__ __forceinline__ Reach reach_of(const cafeq_cache& c, const cafeq_atte
   const RowRange rr = rows_of(a.starts, i, int(a.n));
   r.i = i;
   r.row0 = rr.lo;
-  r.len = tokens_of(c, i);
+  r.len = no_room(c, a.starts) ? 0 : tokens_of(c, i);
   r.pos0 = r.len - (rr.hi - rr.lo);
   r.rows = int(min(int64_t(rr.hi - rr.lo), a.longest)) * rep;
   const int last = min(first + count, r.rows) - 1;

@@ -16,7 +16,7 @@ inline int check_cache(const cafeq_cache* c) {
       int64_t(c->width) * c->block > kMaxKeys)
     return CAFEQ_ERR_UNSUPPORTED;
   if (!aligned_to(c->k, 16) || !aligned_to(c->v, 16) || !aligned_to(c->kscale, 4) || !aligned_to(c->vscale, 4) || !aligned_to(c->table, 4) ||
-      !aligned_to(c->lengths, 4) || !aligned_to(c->refs, 4))
+      !aligned_to(c->lengths, 4) || !aligned_to(c->refs, 4) || !aligned_to(c->missing, 4))
     return CAFEQ_ERR_BAD_ALIGN;
   return CAFEQ_OK;
 }
@@ -30,6 +30,11 @@ __device__ __forceinline__ RowRange rows_of(const int32_t* starts, int i, int n)
   return r;
 }
 __device__ __forceinline__ int tokens_of(const cafeq_cache& c, int i) { return min(max(c.lengths[i], 0), c.width * c.block); }
+// Whether the last reserve found no room: lengths do not count the new tokens then.  (Read without a branch: `any` is readable in any case)
+__device__ __forceinline__ bool no_room(const cafeq_cache& c, const int32_t* any) {
+  const int lack = *(c.missing ? c.missing : any);
+  return c.missing && lack != 0;
+}
 // page of a block of sequence i, or -1
 __device__ __forceinline__ int page_of(const cafeq_cache& c, int i, int block) {
   const int p = c.table[int64_t(i) * c.width + block];

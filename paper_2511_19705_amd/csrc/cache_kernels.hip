@@ -61,12 +61,13 @@ __global__ __launch_bounds__(T) void append_kernel(const AppendArgs a) {
   const int64_t w = blockIdx.x;
   const int i = a.longest == 1 ? int(w) : sequence_of(a.units, a.starts, c.sequences, a.n, w);
   if (i < 0) return;
+  const bool closed = no_room(c, a.starts);
   const RowRange r = rows_of(a.starts, i, a.n);
   const int len = tokens_of(c, i), pos0 = len - (r.hi - r.lo);                 // row lo + j stands at pos0 + j
   const int64_t block = max(pos0, 0) / B + (w - a.units.base(r.lo, i));
   const int64_t first = max(int64_t(pos0), block * B);
   const int64_t last = min(min(int64_t(len), int64_t(pos0) + a.longest), (block + 1) * B);
-  if (first >= last) return;
+  if (first >= last || closed) return;
   const int page = page_of(c, i, int(block));
   if (page < 0) return;
   const int f = int(first - block * B), m = int(last - first), per = d / 8;

@@ -105,6 +105,7 @@ __global__ __launch_bounds__(kScan) void reserve_kernel(const ReserveArgs a) {
   const int lack = over > 0 ? over : max(0, want - found);
   if (tid == 0) {
     *a.missing = lack;
+    if (c.missing) *c.missing = lack;
     a.w.head[0] = lack;
   }
   if (lack) return;
@@ -149,13 +150,13 @@ __global__ __launch_bounds__(kCopy) void copy_shared_kernel(const ReserveArgs a)
   const cafeq_cache& c = a.c;
   const PageWs& w = a.w;
   const int i = blockIdx.x;
-  if (w.head[0] != 0) return;
+  const bool lack = w.head[0] != 0;
   if (a.positions) {
     const RowRange r = rows_of(a.starts, i, a.n);
     const int before = c.lengths[i] - (r.hi - r.lo);
-    for (int e = r.lo + blockIdx.y * kCopy + threadIdx.x; e < r.hi; e += gridDim.y * kCopy) a.positions[e] = before + (e - r.lo);
+    for (int e = r.lo + blockIdx.y * kCopy + threadIdx.x; e < r.hi; e += gridDim.y * kCopy) a.positions[e] = lack ? 0 : before + (e - r.lo);
   }
-  if (w.from[i] < 0) return;
+  if (lack || w.from[i] < 0) return;
   for (int item = blockIdx.y; item < 2 * c.heads; item += gridDim.y) copy_item(c, w.from[i], w.to[i], item);
 }
 
