@@ -831,22 +831,24 @@ def kv_cache(sequences, pages, heads, d, block=64, width=None, device=None):
 
 
 def _cache(c, dev):
-    """(descriptor, its reference for a call, device, scratch of the page calls, addresses) of a KVCache on device number `dev`.  The checks of eight
-    tensors (8 us) are made once, and again where one has another address, or k or the table another shape."""
+    """(descriptor, its reference for a call, device, scratch of the page calls, what the tensors were) of a KVCache on device number `dev`.  The checks of
+    eight tensors (8 us) are made once, and again where one has another address, shape or order."""
     have = c._desc
-    at = (c.k.data_ptr(), c.v.data_ptr(), c.kscale.data_ptr(), c.vscale.data_ptr(), c.table.data_ptr(), c.lengths.data_ptr(), c.refs.data_ptr(),
-          c.missing.data_ptr(), c.k.shape, c.table.shape)
+    k, v, ks, vs, table, lengths, refs, missing = c.k, c.v, c.kscale, c.vscale, c.table, c.lengths, c.refs, c.missing
+    at = (k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), table.data_ptr(), lengths.data_ptr(), refs.data_ptr(), missing.data_ptr(), k.shape, v.shape,
+          table.shape, ks.numel(), vs.numel(), lengths.numel(), refs.numel(), missing.numel(), k.is_contiguous(), v.is_contiguous(), ks.is_contiguous(),
+          vs.is_contiguous(), table.is_contiguous(), lengths.is_contiguous(), refs.is_contiguous(), missing.is_contiguous())
     if have is not None and have[2] == dev and have[4] == at:
         return have
-    if len(c.k.shape) != 4 or len(c.table.shape) != 2:
+    if k.dim() != 4 or table.dim() != 2:
         raise CafeqError("cache: k must be [pages][heads][block][d], table [sequences][width]")
-    pages, heads, block, d = c.k.shape
-    rows, width = c.table.shape
+    pages, heads, block, d = k.shape
+    rows, width = table.shape
     i8, i32, f32 = torch.int8, torch.int32, torch.float32
-    desc = Cache(_operand(c.k, dev, i8, (pages, heads, block, d), "cache.k"), _operand(c.v, dev, i8, (pages, heads, d, block), "cache.v"),
-                 _operand(c.kscale, dev, f32, (pages, heads), "cache.kscale"), _operand(c.vscale, dev, f32, (pages, heads), "cache.vscale"),
-                 _operand(c.table, dev, i32, (rows, width), "cache.table"), _operand(c.lengths, dev, i32, (rows,), "cache.lengths"),
-                 _operand(c.refs, dev, i32, (pages,), "cache.refs"), pages, rows, width, heads, d, block, _operand(c.missing, dev, i32, (1,), "cache.missing"))
+    desc = Cache(_operand(k, dev, i8, (pages, heads, block, d), "cache.k"), _operand(v, dev, i8, (pages, heads, d, block), "cache.v"),
+                 _operand(ks, dev, f32, (pages, heads), "cache.kscale"), _operand(vs, dev, f32, (pages, heads), "cache.vscale"),
+                 _operand(table, dev, i32, (rows, width), "cache.table"), _operand(lengths, dev, i32, (rows,), "cache.lengths"),
+                 _operand(refs, dev, i32, (pages,), "cache.refs"), pages, rows, width, heads, d, block, _operand(missing, dev, i32, (1,), "cache.missing"))
     have = (desc, ctypes.byref(desc), dev, int(lib.cafeq_cache_pages_workspace_bytes(ctypes.byref(desc))), at)
     object.__setattr__(c, "_desc", have)
     return have
@@ -899,15 +901,16 @@ def cache_attend(cache, q, starts, longest=None, scale=None, softcap=0.0, window
     if kind is None:
         raise CafeqError("q must be float32 or bfloat16")
     c, ref = _cache(cache, dev)[:2]
-    if q.dim() != 3 or q.shape[2] != c.d or q.shape[1] < 1 or q.shape[1] % c.heads:
+    shape = q.shape
+    n, hq, d = shape if len(shape) == 3 else (0, 0, 0)
+    if d != c.d or hq < 1 or hq % c.heads:
         raise CafeqError("q must be [n][a multiple of %d][%d]" % (c.heads, c.d))
-    n, hq, d = q.shape
     ldq, hsq = _head_rows(q, dev, "q")
     if out is None:
         out = torch.empty_strided((n, hq, d), (hq * d, d, 1), dtype=q.dtype, device=q.device)
         ldo, hso = hq * d, d
     else:
-        if out.shape != q.shape or out.dtype is not q.dtype:
+        if out.shape != shape or out.dtype is not q.dtype:
             raise CafeqError("out must have the shape and type of q")
         ldo, hso = _head_rows(out, dev, "out")
     sums = torch.empty((n, hq), dtype=torch.float32, device=q.device) if lse else None

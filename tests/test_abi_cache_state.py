@@ -11,3 +11,46 @@ def test_the_place_for_what_lacked(cq):  # noqa: F811
                  lambda f: cq.lib.cafeq_cache_reserve(ctypes.byref(_cache(cq, **f)), FAKE, 1, FAKE, FAKE, FAKE, None)):
         assert call(dict(missing=FAKE + 2)) == ALIGN
     assert _append(cq, dict(missing=FAKE), n=0) == 0 and _attend(cq, dict(missing=FAKE), n=0) == 0
+
+
+def _host_cache(cq, **more):  # noqa: F811
+    """A cache in host memory: its descriptor is made and kept the same way, and nothing is launched."""
+    import torch
+    return torch, cq.kv_cache(3, 20, more.get("heads", 16), more.get("d", 32), block=16, width=4, device=torch.device("cpu"))
+
+
+def _strided(torch, cache):
+    # a table whose rows lie apart takes the place of one whose rows do not: same memory, address and shape
+    base = torch.zeros((3, 8), dtype=torch.int32)
+    cache.table = base.view(-1)[:12].view(3, 4)
+    return lambda: cache.table.set_(base[:, :4])
+
+
+CHANGES = {
+    "v turned": lambda torch, c: lambda: c.v.transpose_(2, 3),
+    "k turned, of the same shape": lambda torch, c: lambda: c.k.transpose_(1, 2),
+    "v viewed": lambda torch, c: lambda: c.v.set_(c.v.view(20, 16, 16, 32)),
+    "k shorter": lambda torch, c: lambda: c.k.set_(c.k[:, :, :, :16]),
+    "fewer pages of v": lambda torch, c: lambda: c.v.set_(c.v[:19]),
+    "lengths shorter": lambda torch, c: lambda: c.lengths.set_(c.lengths[:2]),
+    "refs shorter": lambda torch, c: lambda: c.refs.resize_(7),
+    "scales of k shorter": lambda torch, c: lambda: c.kscale.set_(c.kscale[:3]),
+    "scales of v turned": lambda torch, c: lambda: c.vscale.transpose_(0, 1),
+    "missing empty": lambda torch, c: lambda: c.missing.set_(c.missing[:0]),
+    "rows of the table apart": _strided,
+    "table of another type": lambda torch, c: lambda: setattr(c, "table", c.table.long()),
+}
+
+
+@pytest.mark.parametrize("what", CHANGES)
+def test_a_cache_whose_tensors_change_their_form_is_checked_again(cq, what):  # noqa: F811
+    torch, cache = _host_cache(cq)
+    change = CHANGES[what](torch, cache)
+    kept = cq._cache(cache, -1)
+    assert cq._cache(cache, -1) is kept
+    cache.lengths.add_(3)
+    cache.k.zero_()
+    assert cq._cache(cache, -1) is kept      # contents are free to change
+    change()
+    with pytest.raises(cq.CafeqError):
+        cq._cache(cache, -1)
