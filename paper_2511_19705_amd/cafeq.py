@@ -858,6 +858,15 @@ def _starts(t, rows, dev, what="starts"):
     return _operand(t, dev, torch.int32, (rows + 1,), what)
 
 
+def _bound(longest, n):
+    """The bound on a sequence's rows as 64 bits hold it."""
+    if longest is None:
+        return n
+    if longest < 0:
+        raise CafeqError("longest must be 0 or more")
+    return min(longest, n)
+
+
 def cache_append(cache, k, v, starts, longest=None):
     """cafeq_cache_append: new keys and values [n][heads][d] into the pages of their sequences, in 8 bits.  starts int32 [sequences + 1]: the rows
     of each sequence, the last of its lengths' tokens; longest: an upper bound of a sequence's rows (n, if not given).  Behind a cache_reserve
@@ -872,7 +881,7 @@ def cache_append(cache, k, v, starts, longest=None):
     (ldk, hsk), (ldv, hsv) = _head_rows(k, dev, "k"), _head_rows(v, dev, "v")
     ps = _starts(starts, c.sequences, dev)
     if n:
-        rc = lib.cafeq_cache_append(ref, k.data_ptr(), v.data_ptr(), kind, n, ldk, hsk, ldv, hsv, ps, n if longest is None else longest,
+        rc = lib.cafeq_cache_append(ref, k.data_ptr(), v.data_ptr(), kind, n, ldk, hsk, ldv, hsv, ps, _bound(longest, n),
                                     torch._C._cuda_getCurrentRawStream(dev))
         if rc:
             _check(rc)
@@ -905,6 +914,8 @@ def cache_attend(cache, q, starts, longest=None, scale=None, softcap=0.0, window
     n, hq, d = shape if len(shape) == 3 else (0, 0, 0)
     if d != c.d or hq < 1 or hq % c.heads:
         raise CafeqError("q must be [n][a multiple of %d][%d]" % (c.heads, c.d))
+    if not 0 <= window < 1 << 31:
+        raise CafeqError("window must be 0 .. 2^31 - 1")
     ldq, hsq = _head_rows(q, dev, "q")
     if out is None:
         out = torch.empty_strided((n, hq, d), (hq * d, d, 1), dtype=q.dtype, device=q.device)
@@ -914,7 +925,7 @@ def cache_attend(cache, q, starts, longest=None, scale=None, softcap=0.0, window
             raise CafeqError("out must have the shape and type of q")
         ldo, hso = _head_rows(out, dev, "out")
     sums = torch.empty((n, hq), dtype=torch.float32, device=q.device) if lse else None
-    a = Attention(q.data_ptr(), out.data_ptr(), None if sums is None else sums.data_ptr(), n, ldq, hsq, ldo, hso, n if longest is None else longest,
+    a = Attention(q.data_ptr(), out.data_ptr(), None if sums is None else sums.data_ptr(), n, ldq, hsq, ldo, hso, _bound(longest, n),
                   _starts(starts, c.sequences, dev), kind, hq, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, softcap)
     if n:
         stream = torch._C._cuda_getCurrentRawStream(dev)
