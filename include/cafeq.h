@@ -354,7 +354,7 @@ int cafeq_cache_values(const cafeq_cache* cache, const int32_t* begin, const int
  * largest, weighed with the scale of v, to multiples of 2^-39 of it); with float32 both are taken in two such parts.  Sums are float32 in a fixed order.  A row of q that holds a NaN or an infinity gives NaN.  A page and head of v with a scale below 2^-100 counts as zeros;
  * where scales of a head lie more than 2^100 apart the weight of the smaller ones' keys may be lost.
  * Rows start at multiples of 16 bytes; out overlaps no input.  longest as in cafeq_cache_append (rows beyond it are left).
- * heads_q a multiple of heads, up to 4096; n up to 2^24, n * heads_q below 2^31.  ws: cafeq_cache_attend_workspace_bytes() bytes (may be 0), 16-byte aligned. */
+ * heads_q a multiple of heads, up to 4096; n up to 2^24, n * heads_q below 2^31, and what a launch holds: 2 n heads_q + 512 sequences heads below 2^32 is always taken.  ws: cafeq_cache_attend_workspace_bytes() bytes (may be 0), 16-byte aligned. */
 typedef struct {
   const void* q;
   void* out;

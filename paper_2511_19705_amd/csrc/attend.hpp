@@ -67,7 +67,7 @@ __device__ __forceinline__ Reach reach_of(const cafeq_cache& c, const cafeq_atte
   r.len = no_room(c, a.starts) ? 0 : tokens_of(c, i);
   r.pos0 = r.len - (rr.hi - rr.lo);
   r.rows = int(min(int64_t(rr.hi - rr.lo), a.longest)) * rep;
-  const int last = min(first + count, r.rows) - 1;
+  const int last = int(min(unsigned(first) + unsigned(count), unsigned(r.rows))) - 1;
   r.lo = key_begin(a, r.pos0 + first / rep);
   r.hi = last < first ? 0 : key_end(a, r.len, r.pos0 + last / rep);
   return r;

@@ -39,6 +39,8 @@ struct AttendPlans {
   int64_t few_tiles, many_tiles;
   size_t few_sums, few_parts, many_sums, many_parts;
   size_t bytes() const { return few_sums + few_parts + many_sums + many_parts; }
+  // a launch's first dimension holds less than 2^32 threads
+  bool fits() const { return !many || many_tiles * m.c.heads * 64 * many_waves(m.a.dtype, (m.c.d + 63) / 64) <= int64_t(UINT32_MAX); }
 };
 
 AttendPlan plan_few(const cafeq_cache& c, const cafeq_attention& a, int64_t rows, int64_t room) {
@@ -113,7 +115,8 @@ extern "C" {
 
 size_t cafeq_cache_attend_workspace_bytes(const cafeq_cache* cache, const cafeq_attention* a) {
   if (check_attention(cache, a) || a->n == 0 || a->longest == 0 || cache->sequences == 0) return 0;
-  return plan(*cache, *a).bytes();
+  const AttendPlans s = plan(*cache, *a);
+  return s.fits() ? s.bytes() : 0;
 }
 
 int cafeq_cache_attend(const cafeq_cache* cache, const cafeq_attention* a, void* ws, void* stream) {
@@ -122,6 +125,7 @@ int cafeq_cache_attend(const cafeq_cache* cache, const cafeq_attention* a, void*
   if (!aligned_to(ws, 16)) return CAFEQ_ERR_BAD_ALIGN;
   if (a->n == 0 || a->longest == 0 || cache->sequences == 0) return CAFEQ_OK;
   AttendPlans s = plan(*cache, *a);
+  if (!s.fits()) return CAFEQ_ERR_UNSUPPORTED;
   if (s.bytes() && !ws) return CAFEQ_ERR_WORKSPACE;
   char* at = static_cast<char*>(ws);
   s.f.sums = reinterpret_cast<float*>(at);

@@ -45,7 +45,8 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
   const int64_t w = (gridDim.x - 1 - blockIdx.x) / c.heads;
   const int i = sequence_of(p.units, a.starts, c.sequences, int(a.n), w);
   if (i < 0) return;
-  const int first = int(w - p.units.base(min(max(a.starts[i], 0), int(a.n)), i)) * kTile;
+  // (starts out of order may put it anywhere: rows are below 2^31)
+  const int first = int(min(w - p.units.base(min(max(a.starts[i], 0), int(a.n)), i), int64_t(INT32_MAX / kTile))) * kTile;
   const Reach r = reach_of(c, a, i, p.rep, first, kTile);
   if (first >= r.rows || r.rows <= p.few_rows) return;
   const int c0 = r.lo / KT, c1 = max(c0, (r.hi + KT - 1) / KT), used = max(1, (c1 - c0 + p.span - 1) / p.span);
@@ -412,7 +413,7 @@ __global__ __launch_bounds__(kJoin) void attend_many_join_kernel(const AttendPla
   const int64_t w = blockIdx.x / c.heads;
   const int i = sequence_of(p.units, p.a.starts, c.sequences, int(p.a.n), w);
   if (i < 0) return;
-  const int first = int(w - p.units.base(min(max(p.a.starts[i], 0), int(p.a.n)), i)) * kTile;
+  const int first = int(min(w - p.units.base(min(max(p.a.starts[i], 0), int(p.a.n)), i), int64_t(INT32_MAX / kTile))) * kTile;
   const Reach r = reach_of(c, p.a, i, p.rep, first, kTile);
   if (first >= r.rows || r.rows <= p.few_rows) return;
   const int c0 = r.lo / KT, c1 = max(c0, (r.hi + KT - 1) / KT), used = (c1 - c0 + p.span - 1) / p.span;

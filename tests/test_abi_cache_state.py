@@ -3,7 +3,7 @@ import ctypes
 
 import pytest
 
-from tests.test_abi_cache import ALIGN, FAKE, _attend, _append, _cache, cq  # noqa: F401
+from tests.test_abi_cache import ALIGN, FAKE, UNSUPPORTED, _attend, _append, _cache, cq  # noqa: F401
 
 
 def test_the_place_for_what_lacked(cq):  # noqa: F811
@@ -54,3 +54,11 @@ def test_a_cache_whose_tensors_change_their_form_is_checked_again(cq, what):  # 
     change()
     with pytest.raises(cq.CafeqError):
         cq._cache(cache, -1)
+
+
+@pytest.mark.parametrize("heads,heads_q,n,sequences,d", [(257, 257, 100, 65535, 128), (1, 128, (1 << 24) - 1, 2, 16), (1, 1024, (1 << 21) - 1, 9, 64), (4096, 4096, 128, 4096, 256)])
+def test_more_threads_than_a_launch_holds(cq, heads, heads_q, n, sequences, d):  # noqa: F811
+    cache = dict(heads=heads, sequences=sequences, d=d)
+    far = dict(ldq=1 << 20, ldo=1 << 20, hsq=d, hso=d, heads_q=heads_q, n=n, longest=n, out=1 << 46, dtype=1)
+    assert _attend(cq, cache, size=True, **far) == 0
+    assert _attend(cq, cache, ws=FAKE, **far) == UNSUPPORTED
