@@ -346,7 +346,7 @@ int cafeq_cache_values(const cafeq_cache* cache, const int32_t* begin, const int
 
 /* Attention of the new tokens over the cache.  Row j of sequence i stands at position p = lengths[i] - (starts[i+1] - starts[i]) + j; query
  * head h reads key head h / (heads_q / heads):
- *   x_t = scale q . K_t, with softcap > 0: softcap tanh(x_t / softcap);  keys t: 0 <= t < lengths[i], t <= p if causal, t > p - window if window > 0
+ *   x_t = scale q . K_t, with 0 < softcap <= 2^100: softcap tanh(x_t / softcap);  keys t: 0 <= t < lengths[i], t <= p if causal, t > p - window if window > 0
  *   out = sum_t exp(x_t) V_t / sum_t exp(x_t),  lse = log sum_t exp(x_t)   (a row without keys: 0 and -inf)
  * Scores are float32 numbers of any magnitude up to 2^126 (a row whose largest passes 2^126 is not specified); from 2^12 on a row may take them against a whole number near its largest.
  * K, V: the codes times their scales, which are not negative.  q, out float32 or bfloat16 (dtype); lse float32 [n][heads_q] dense or NULL.  Queries of bfloat16 are

@@ -48,6 +48,15 @@ __device__ __forceinline__ float capped(float z, float out) {
   if constexpr (F32) return tanhf(z) * out;
   else return fmaf(-2.f * out, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z)), out);
 }
+// The same for results of bfloat16 under a cap so far above the scores (kWideCap) that 2^-22 of it is more than a score is known to: below a quarter tanh's
+// series (the first term left out is below 2^-26 of it), and so good to 2^-20 of itself everywhere.  Float32's tanh serves all caps.
+constexpr float kWideCap = 256.f, kNoCap = 0x1p100f;
+enum Cap { kCapNone, kCapNear, kCapWide };
+__device__ __forceinline__ float capped_wide(float z, float out) {
+  const float u = z * (0.5f * kLn2), s = u * u;
+  const float series = u * fmaf(s, fmaf(s, fmaf(s, fmaf(s, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+  return fabsf(u) < 0.25f ? series * out : capped<false>(z, out);
+}
 
 // The rows of one tile and what of the keys they reach.  Row R of a sequence and key head is token R / rep, query head R % rep of the group.
 struct Reach {
@@ -133,6 +142,8 @@ struct AttendPlan {
   int tiles;          // row tiles of a sequence
   int splits, span;   // parts that the keys of a tile may be cut into, steps of 32 keys (attend_many: tiles of keys) in each
   int keep;           // rows of a tile that have room in the parts
+  int cap;
+  float cap_in, cap_out;      // a score (in log2) under the soft cap: cap_out tanh(score cap_in), cap_in times 2 log2 e for bfloat16
   float* sums;        // parts [sequence][tile][head][split][keep]: (M, sum of weights)
   float* parts;       // and [keep][d]
 };

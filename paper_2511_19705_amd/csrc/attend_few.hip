@@ -207,16 +207,16 @@ __global__ __launch_bounds__(kThreads, Tag::dtype == CAFEQ_F32 && DB == 4 ? 1 : 
       }
     }
     if (next < end) load_k(next);
-    bool far = false;      // whether scores may be large
+    bool far = p.cap == kCapWide;      // whether scores may be large, or take the cap of large ones
 #pragma unroll
     for (int n = 0; n < NS; ++n) far |= f[n] > near_factor(DB);
-    if (a.softcap > 0.f) {
-      const float in = kF32 ? 1.f / a.softcap : 2.f * kLog2e * __builtin_amdgcn_rcpf(a.softcap), out = a.softcap * kLog2e;
-      far &= out > kFar;
+    if (p.cap == kCapNear) {
+      far &= p.cap_out > kFar;
 #pragma unroll
       for (int n = 0; n < NS; ++n) {
+        const float in = f[n] * p.cap_in;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[n][e >> 2][e & 3] = capped<kF32>(x[n][e >> 2][e & 3] * (f[n] * in), out);
+        for (int e = 0; e < 8; ++e) x[n][e >> 2][e & 3] = capped<kF32>(x[n][e >> 2][e & 3] * in, p.cap_out);
         f[n] = 1.f;
       }
     }
@@ -233,6 +233,15 @@ __global__ __launch_bounds__(kThreads, Tag::dtype == CAFEQ_F32 && DB == 4 ? 1 : 
         top = fmaxf(top, t + s[n].exp);
       }
     } else {
+      if (p.cap == kCapWide) {
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+          const float in = f[n] * p.cap_in;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[n][e >> 2][e & 3] = capped_wide(x[n][e >> 2][e & 3] * in, p.cap_out);
+          f[n] = 1.f;
+        }
+      }
       if (based || far) {
         float most = kNoKey;
 #pragma unroll

@@ -43,8 +43,20 @@ struct AttendPlans {
   bool fits() const { return !many || many_tiles * m.c.heads * 64 * many_waves(m.a.dtype, (m.c.d + 63) / 64) <= int64_t(UINT32_MAX); }
 };
 
-AttendPlan plan_few(const cafeq_cache& c, const cafeq_attention& a, int64_t rows, int64_t room) {
+AttendPlan plan_of(const cafeq_cache& c, const cafeq_attention& a) {
   AttendPlan p{c, a, a.heads_q / c.heads, __builtin_ctz(unsigned(c.block))};
+  if (a.softcap > 0.f) {
+    // a cap below 2^-30 leaves every score within 2^-30 of 0, however steep the way there
+    const float in = std::min(1.f / a.softcap, 0x1p30f);
+    p.cap = a.dtype != CAFEQ_F32 && a.softcap > kWideCap ? kCapWide : kCapNear;
+    p.cap_in = a.dtype == CAFEQ_F32 ? in : 2.f * kLog2e * in;
+    p.cap_out = a.softcap * kLog2e;
+  }
+  return p;
+}
+
+AttendPlan plan_few(const cafeq_cache& c, const cafeq_attention& a, int64_t rows, int64_t room) {
+  AttendPlan p = plan_of(c, a);
   p.few_rows = int(std::min<int64_t>(rows, INT32_MAX));
   p.tiles = int((rows + 15) / 16);
   p.keep = int(std::min<int64_t>(16, rows));
@@ -67,7 +79,7 @@ AttendPlan plan_few(const cafeq_cache& c, const cafeq_attention& a, int64_t rows
 }
 
 AttendPlan plan_many(const cafeq_cache& c, const cafeq_attention& a, int64_t few_rows, int64_t room) {
-  AttendPlan p{c, a, a.heads_q / c.heads, __builtin_ctz(unsigned(c.block))};
+  AttendPlan p = plan_of(c, a);
   const int db = (c.d + 63) / 64, tile = 32 * many_waves(a.dtype, db), kt = many_keys(a.dtype, db);
   p.few_rows = int(few_rows);
   p.units = Units{p.rep, tile, 1};
@@ -86,6 +98,7 @@ AttendPlans plan(const cafeq_cache& c, const cafeq_attention& given) {
   AttendPlans s{};
   cafeq_attention a = given;
   a.longest = std::min(a.longest, a.n);
+  if (a.softcap > kNoCap) a.softcap = 0.f;      // bounds nothing: float32 scores below 2^88 keep their bits under it
   if (a.window >= kMaxKeys) a.window = 0;      // reaches all keys: no position is further from the first
   const int64_t rep = a.heads_q / c.heads, rows = a.longest * rep, room = int64_t(c.width) * c.block;
   const int64_t few = few_rows(c);

@@ -184,14 +184,14 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
   float M[QT], l[QT];
   float* row_lds = reinterpret_cast<float*>(buf + 2 * kBuf) + tid;
   auto row = [&](int t, int what) -> float& { return row_lds[(what * QT + t) * kThreads]; };
-  // scales of k (their bits) from which on scores of the wave's rows may be large; 0 once a row has a reference
+  // scales of k (their bits) from which on scores of the wave's rows may be large, or take the cap of large ones; 0 once a row has a reference
   float most_unit = 0.f;
 #pragma unroll
   for (int t = 0; t < QT; ++t) most_unit = fmaxf(most_unit, unit[t]);
 #pragma unroll
   for (int k = 1; k < 32; k <<= 1) most_unit = fmaxf(most_unit, __shfl_xor(most_unit, k));
-  const bool bounded = a.softcap > 0.f && a.softcap * kLog2e <= kFar;
-  const uint32_t near_scale = __builtin_amdgcn_readfirstlane(bounded ? 0xFFFFFFFFu : max(1u, __float_as_uint(near_factor(DB) / most_unit)));
+  const uint32_t near_scale = __builtin_amdgcn_readfirstlane(p.cap == kCapWide ? 1u : p.cap == kCapNear && p.cap_out <= kFar ? 0xFFFFFFFFu :
+                                                             max(1u, __float_as_uint(near_factor(DB) / most_unit)));
   uint32_t far_scale = near_scale;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -264,10 +264,9 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
         float f[kRuns];
 #pragma unroll
         for (int k = 0; k < kRuns; ++k) f[k] = unit[t] * ksc[k];
-        if (a.softcap > 0.f) {
-          const float in = kF32 ? 1.f / a.softcap : 2.f * kLog2e * __builtin_amdgcn_rcpf(a.softcap), out = a.softcap * kLog2e;
+        if (p.cap == kCapNear) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[t][e] = capped<kF32>(x[t][e] * (f[e / kRun] * in), out);
+          for (int e = 0; e < 16; ++e) x[t][e] = capped<kF32>(x[t][e] * (f[e / kRun] * p.cap_in), p.cap_out);
 #pragma unroll
           for (int k = 0; k < kRuns; ++k) f[k] = 1.f;
         }
@@ -288,6 +287,12 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
           }
         } else {
           if (__builtin_expect(far, 0)) {
+            if (p.cap == kCapWide) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) x[t][e] = capped_wide(x[t][e] * (f[e / kRun] * p.cap_in), p.cap_out);
+#pragma unroll
+              for (int k = 0; k < kRuns; ++k) f[k] = 1.f;
+            }
             float high = kNoKey;
 #pragma unroll
             for (int e = 0; e < 16; ++e) high = int(in(e)) & int(!sc[e / kRun].zero) ? fmaxf(high, x[t][e] * f[e / kRun]) : high;

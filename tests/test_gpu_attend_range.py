@@ -1,6 +1,7 @@
 """GPU: numbers at the ends of what the attention call takes, and beyond them."""
 import pytest
 
+from tests import cache_ref as R
 from tests.test_gpu_attend import _cache, _starts
 
 pytestmark = pytest.mark.gpu
@@ -39,3 +40,31 @@ def test_integers_that_32_or_64_bits_do_not_hold(env, counts):
         for call in (lambda: cafeq.cache_attend(cache, q, starts, longest=longest), lambda: cafeq.cache_append(cache, k, k, starts, longest=longest)):
             with pytest.raises(cafeq.CafeqError):
                 call()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cap", [200.0, 1e3, 1e4, 1e6, 1e12, 1e30, 3e38, 1e-3, 1e-9, 1e-20, 1e-38, 1e-44])
+def test_soft_caps_of_any_size(env, dtype, cap):
+    """Scores of a few units and of hundreds under caps far above and below them.  Tolerance for each element as derived in test_gpu_attend; its bound on the
+    2-norm besides, 3e-6, is one of scores near one: here each is off by up to 8 u of hundreds, 2^-13, which goes into the weights as it is."""
+    torch, _ = env
+    for counts, lengths in (([1, 3], [300, 200]), ([90, 2], [300, 200])):
+        for d in (64, 256):
+            cache, q, starts = _problem(env, counts, lengths, dtype, d=d)
+            for scale in (d ** -0.5, 20.0):
+                out, lse = env[1].cache_attend(cache, q, starts, softcap=cap, scale=scale, lse=True)
+                want, wlse, W, size, floor = R.attend(torch, cache, q, _starts(counts), scale, cap, 0, True)
+                u, N, f32 = 2.0 ** -24, 300, dtype == "f32"
+                e = 2 * (((2 * d + 16) * u + 2.0 ** -22) * size) + 4 * u
+                tol = (2 * e + (2.0 ** -22 if f32 else 2.0 ** -12) + (N + 16) * u)[:, :, None] * W + (0 if f32 else 2.0 ** -8) * want.abs() + 2.0 ** -38 * floor
+                assert ((out.double() - want).abs() <= tol + 1e-37).all()
+                assert ((lse.double() - wlse).abs() <= 2 * e + (N + 16) * u + 8 * u * wlse.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_an_infinite_soft_cap_is_none(env, dtype):
+    torch, cafeq = env
+    for counts in ([1, 3], [90, 2]):
+        cache, q, starts = _problem(env, counts, [300, 200], dtype)
+        got, want = (cafeq.cache_attend(cache, q, starts, softcap=c, lse=True) for c in (float("inf"), 0.0))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
