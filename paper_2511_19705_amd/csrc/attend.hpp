@@ -20,6 +20,7 @@ using f32x16_t = __attribute__((__vector_size__(16 * sizeof(float)))) float;
 
 constexpr float kNoKey = -FLT_MAX;       // M before the first key
 constexpr float kTop = 14.f;              // log2 of the largest p
+constexpr int kRoom = 17;                 // the sum of weights, p 2^-exp, is held in units of 2^(M + kRoom): 2^30 keys of p = 2^14 fit with exp = -100
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kZeroScale = 0x1p-100f;  // pages of v below it hold zeros: their keys have weight, and no value
 
@@ -82,7 +83,7 @@ __device__ __forceinline__ Reach reach_of(const cafeq_cache& c, const cafeq_atte
   return r;
 }
 
-// A page's scale of v as mant 2^exp; inv = 2^-exp.  A scale that is no number is its own mantissa.
+// A page's scale of v as mant 2^exp; inv = 2^-(exp + kRoom).  A scale that is no number is its own mantissa.
 struct ValueScale { float exp, mant, inv; bool zero; };
 __device__ __forceinline__ ValueScale value_scale(float vs) {
   ValueScale s;
@@ -91,7 +92,7 @@ __device__ __forceinline__ ValueScale value_scale(float vs) {
   const bool plain = e < 255 && !s.zero;
   s.exp = plain ? float(int(e) - 127) : 0.f;
   s.mant = plain ? __uint_as_float((u & 0x7FFFFFu) | 0x3F800000u) : s.zero ? 0.f : vs;
-  s.inv = plain ? __uint_as_float((254u - e) << 23) : 1.f;
+  s.inv = ldexpf(1.f, (plain ? 127 - int(e) : 0) - kRoom);
   return s;
 }
 
@@ -107,11 +108,11 @@ __device__ __forceinline__ float next_base(float top, float base, bool first) {
   const bool leaves = base != 0.f ? top > base : fabsf(top) > kLarge && (top > 0.f || first);
   return leaves && top > kNoKey ? ceilf(top) : base;
 }
-// What a wave's o and l are times in the end, and the M that they are then in units of: a float32 of its own again, base + M, however far it is
-struct Finish { float all, unit; };
+// What a wave's o and l are times in the end, and the M that they are then in units of: a float32 of its own again, base + M + kRoom, however far it is
+struct Finish { float all, unit, sum_unit; };
 __device__ __forceinline__ Finish finish_of(float M, float base) {
-  const float all = base + M;
-  return {all, __builtin_amdgcn_exp2f(M - (all - base))};
+  const float all = base + (M + kRoom), unit = __builtin_amdgcn_exp2f(M - (all - base));
+  return {all, unit, unit * float(1 << kRoom)};
 }
 
 // Rows of q are taken times a power of two that brings the largest magnitude (its bits) to [2^14, 2^15): bfloat16 then is exact in float16 down to

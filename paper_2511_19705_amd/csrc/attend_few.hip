@@ -339,7 +339,7 @@ __global__ __launch_bounds__(kThreads, Tag::dtype == CAFEQ_F32 && DB == 4 ? 1 : 
   lz = sum_across(lz);
   const Finish fin = finish_of(M, based ? base_lds[wave * kTile + l16] : 0.f);
   const float both = fmaxf(fin.all, mz);
-  l = l * (fin.unit * __builtin_amdgcn_exp2f(fin.all - both)) + lz * __builtin_amdgcn_exp2f(mz - both);
+  l = l * (fin.sum_unit * __builtin_amdgcn_exp2f(fin.all - both)) + lz * __builtin_amdgcn_exp2f(mz - both);
   if (g == 0) *reinterpret_cast<float2*>(sum_lds + 2 * (wave * kTile + l16)) = make_float2(both, l);
   __syncthreads();
   float top = kNoKey;

@@ -392,8 +392,8 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
     const int place = wave * 32 * QT + 32 * t + l32, R = first + place;
     float sum = l[t] + __shfl_xor(l[t], 32), lz = row(t, kZeroSum), sumz = lz + __shfl_xor(lz, 32), mz = row(t, kZeroMax);
     const Finish fin = finish_of(M[t], far_scale == 0u ? row(t, kBase) : 0.f);
-    const float both = fmaxf(fin.all, mz), own = fin.unit * __builtin_amdgcn_exp2f(fin.all - both);
-    const float total = sum * own + sumz * __builtin_amdgcn_exp2f(mz - both);
+    const float both = fmaxf(fin.all, mz), near = __builtin_amdgcn_exp2f(fin.all - both), own = fin.unit * near;
+    const float total = sum * (fin.sum_unit * near) + sumz * __builtin_amdgcn_exp2f(mz - both);
     if (R >= r.rows) continue;
 #pragma unroll
     for (int m = 0; m < MT; ++m)

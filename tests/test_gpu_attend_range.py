@@ -68,3 +68,26 @@ def test_an_infinite_soft_cap_is_none(env, dtype):
         cache, q, starts = _problem(env, counts, [300, 200], dtype)
         got, want = (cafeq.cache_attend(cache, q, starts, softcap=c, lse=True) for c in (float("inf"), 0.0))
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("power", [-99, -90, -60, 60, 100, 115])
+def test_many_keys_of_equal_weight_at_the_ends_of_the_scales(env, dtype, power):
+    """Scores of 0 over 70000 keys whose v has scales near 2^power: the mean of V, and the logarithm of their number.  All weights are equal, so that only their sums
+    round: a lane adds at most 70000 / 4 of them one after another, waves and parts less than 512 on top, each addition within 2^-24, to the nearest; their errors are
+    of either sign, and 2^-14 is 2^10 of them in one direction.  Weights 2^-11 more for bfloat16, as in test_gpu_attend_scores, results 2^-8 of themselves."""
+    torch, cafeq = env
+    N = 70000
+    for n in (1, 100):
+        cache, q, starts = _problem(env, [n], [N], dtype)
+        cache.vscale.copy_(2.0 ** power * (1 + torch.rand(cache.vscale.shape, device="cuda:0")))
+        out, lse = cafeq.cache_attend(cache, q * 0, starts, lse=True)
+        keys = torch.arange(N - n + 1, N + 1, device="cuda:0").double()
+        assert ((lse.double() - torch.log(keys)[:, None]).abs() <= 2.0 ** -14).all()
+        page = cache.table[0, :-(-N // 32)].long()
+        for h in range(2):
+            V = (cache.v[page, h].double().transpose(1, 2) * cache.vscale[page, h].double()[:, None, None]).reshape(-1, 64)[:N]
+            want, W = V.cumsum(0)[N - n:] / keys[:, None], V.abs().cumsum(0)[N - n:] / keys[:, None]
+            for g in (2 * h, 2 * h + 1):
+                tol = (2.0 ** -14 if dtype == "f32" else 2.0 ** -11 + 2.0 ** -14) * W + (0.0 if dtype == "f32" else 2.0 ** -8) * want.abs()
+                assert ((out[:, g].double() - want).abs() <= tol).all()
