@@ -92,7 +92,8 @@ __device__ __forceinline__ ValueScale value_scale(float vs) {
   const bool plain = e < 255 && !s.zero;
   s.exp = plain ? float(int(e) - 127) : 0.f;
   s.mant = plain ? __uint_as_float((u & 0x7FFFFFu) | 0x3F800000u) : s.zero ? 0.f : vs;
-  s.inv = ldexpf(1.f, (plain ? 127 - int(e) : 0) - kRoom);
+  // (put together as bits, which the scalar unit does for a wave; subnormal for the largest scales)
+  s.inv = !plain ? 1.f / float(1 << kRoom) : __uint_as_float(e < 254u - kRoom ? (254u - kRoom - e) << 23 : 1u << (276u - kRoom - e));
   return s;
 }
 
