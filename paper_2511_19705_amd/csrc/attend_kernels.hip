@@ -70,7 +70,7 @@ AttendPlan plan_few(const cafeq_cache& c, const cafeq_attention& a, int64_t rows
   int64_t part = std::min<int64_t>(2048, std::max<int64_t>(128, keys * groups / 512));
   while (part > 512 && keys * groups / part < 1024) part /= 2;
   // room that sequences do not use is cut too, into workgroups that end at once: not too many of them
-  while (keys * groups / part > 16384) part *= 2;
+  while (part < keys && keys * groups / part > 16384) part *= 2;
   p.span = int((part + 31) / 32);
   p.span = std::max<int>(p.span, int((keys + int64_t(32) * 65535 - 1) / (int64_t(32) * 65535)));      // a grid's second dimension
   p.splits = int((keys + 32 * int64_t(p.span) - 1) / (32 * int64_t(p.span)));

@@ -62,3 +62,11 @@ def test_more_threads_than_a_launch_holds(cq, heads, heads_q, n, sequences, d): 
     far = dict(ldq=1 << 20, ldo=1 << 20, hsq=d, hso=d, heads_q=heads_q, n=n, longest=n, out=1 << 46, dtype=1)
     assert _attend(cq, cache, size=True, **far) == 0
     assert _attend(cq, cache, ws=FAKE, **far) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("heads,sequences", [(4096, 65535), (7, 65535), (4096, 60000)])
+def test_room_that_no_sequence_fills_takes_no_workspace(cq, heads, sequences):  # noqa: F811
+    """2^30 tokens of room a sequence: more parts than a launch should have are not cut, nor room for them asked."""
+    cache = dict(heads=heads, sequences=sequences, d=16, width=1 << 26)
+    size = _attend(cq, cache, size=True, heads_q=heads, n=10, longest=1, ldq=1 << 20, ldo=1 << 20, hsq=16, hso=16, out=1 << 46)
+    assert size <= 16384 * 4 * 16 * (16 + 2) * 4
