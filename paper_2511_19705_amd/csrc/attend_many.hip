@@ -32,8 +32,8 @@ template <class Tag, int DB, bool EXACT, bool ONE>
 __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag::dtype, DB)) void attend_many_kernel(const AttendPlan p) {
   using elem = typename Tag::elem;
   constexpr bool kF32 = Tag::dtype == CAFEQ_F32;
-  constexpr int QT = 1, kWaves = many_waves(Tag::dtype, DB), kThreads = 64 * kWaves, kParts = kF32 ? 2 : 1, KT = many_keys(Tag::dtype, DB), NT = KT / 32, KS = 4 * DB, MT = 2 * DB, U = KT / 16;
-  constexpr int kTile = 32 * QT * kWaves, E = (KT * KS + kThreads - 1) / kThreads;
+  constexpr int kWaves = many_waves(Tag::dtype, DB), kThreads = 64 * kWaves, kParts = kF32 ? 2 : 1, KT = many_keys(Tag::dtype, DB), NT = KT / 32;
+  constexpr int KS = 4 * DB, MT = 2 * DB, U = KT / 16, kTile = 32 * kWaves, E = (KT * KS + kThreads - 1) / kThreads;
   constexpr int kRunK = KT + 1, kRunV = 64 * DB + 1, kBufK = 2 * KS * kRunK, kBuf = kBufK + 2 * U * kRunV;
   extern __shared__ __align__(16) half8_t buf[];
   const cafeq_cache& c = p.c;
@@ -54,52 +54,44 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
   const int begin = c0 + split * p.span, end = min(c1, begin + p.span);
 
   // rows of the wave
-  const int wfirst = first + wave * 32 * QT, wlast = min(wfirst + 32 * QT, r.rows) - 1;
+  const int wfirst = first + wave * 32, wlast = min(wfirst + 32, r.rows) - 1;
   const int wlo = key_begin(a, r.pos0 + wfirst / p.rep), whi = wlast < wfirst ? 0 : key_end(a, r.len, r.pos0 + wlast / p.rep);
   const int all_lo = key_begin(a, r.pos0 + max(wlast, 0) / p.rep), all_hi = key_end(a, r.len, r.pos0 + wfirst / p.rep);
-  int klo[QT], khi[QT];
-  half8_t q[kParts][QT][KS];
-  float unit[QT];
+  half8_t q[kParts][KS];
+  const int mine = wfirst + l32, token = mine / p.rep, pos = r.pos0 + token;
+  const bool live = mine < r.rows;
+  const int klo = live ? key_begin(a, pos) : 0, khi = live ? key_end(a, r.len, pos) : 0;
+  const elem* qrow = static_cast<const elem*>(a.q) + int64_t(r.row0 + (live ? token : 0)) * a.ldq + int64_t(head * p.rep + (live ? mine - token * p.rep : 0)) * a.hsq;
+  float v[KS][8];
+  uint32_t bits = 0;
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const int R = wfirst + 32 * t + l32, token = R / p.rep;
-    const bool live = R < r.rows;
-    const int pos = r.pos0 + token;
-    klo[t] = live ? key_begin(a, pos) : 0;
-    khi[t] = live ? key_end(a, r.len, pos) : 0;
-    const elem* x = static_cast<const elem*>(a.q) + int64_t(r.row0 + (live ? token : 0)) * a.ldq + int64_t(head * p.rep + (live ? R - token * p.rep : 0)) * a.hsq;
-    float v[KS][8];
-    uint32_t bits = 0;
+  for (int s = 0; s < KS; ++s) {
+    const bool in = live && (EXACT || 16 * s < d);
+    const elem* y = qrow + (EXACT || 16 * s < d ? 16 * s + 8 * h : 0);
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const bool in = live && (EXACT || 16 * s < d);
-      const elem* y = x + (EXACT || 16 * s < d ? 16 * s + 8 * h : 0);
-#pragma unroll
-      for (int e = 0; e < 8; e += 4) {
-        const float4 f = load4(y + e);
-        v[s][e] = in ? f.x : 0.f; v[s][e + 1] = in ? f.y : 0.f; v[s][e + 2] = in ? f.z : 0.f; v[s][e + 3] = in ? f.w : 0.f;
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) bits = max(bits, __float_as_uint(v[s][e]) & 0x7FFFFFFFu);
+    for (int e = 0; e < 8; e += 4) {
+      const float4 f = load4(y + e);
+      v[s][e] = in ? f.x : 0.f; v[s][e + 1] = in ? f.y : 0.f; v[s][e + 2] = in ? f.z : 0.f; v[s][e + 3] = in ? f.w : 0.f;
     }
-    bits = max(bits, uint32_t(__shfl_xor(int(bits), 32)));
-    const QueryScale qs = query_scale(bits, a);
-    unit[t] = qs.unit;
 #pragma unroll
-    for (int s = 0; s < KS; ++s)
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const float f0 = v[s][e] * qs.up, f1 = v[s][e + 1] * qs.up;
-        const half2_t x2 = to_half(f0, f1);
-        q[0][t][s][e] = x2[0];
-        q[0][t][s][e + 1] = x2[1];
-        if constexpr (kF32) {
-          const half2_t y2 = to_half(f0 - float(x2[0]), f1 - float(x2[1]));
-          q[1][t][s][e] = y2[0];
-          q[1][t][s][e + 1] = y2[1];
-        }
-      }
+    for (int e = 0; e < 8; ++e) bits = max(bits, __float_as_uint(v[s][e]) & 0x7FFFFFFFu);
   }
+  bits = max(bits, uint32_t(__shfl_xor(int(bits), 32)));
+  const QueryScale qs = query_scale(bits, a);
+#pragma unroll
+  for (int s = 0; s < KS; ++s)
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const float f0 = v[s][e] * qs.up, f1 = v[s][e + 1] * qs.up;
+      const half2_t x2 = to_half(f0, f1);
+      q[0][s][e] = x2[0];
+      q[0][s][e + 1] = x2[1];
+      if constexpr (kF32) {
+        const half2_t y2 = to_half(f0 - float(x2[0]), f1 - float(x2[1]));
+        q[1][s][e] = y2[0];
+        q[1][s][e + 1] = y2[1];
+      }
+    }
 
   // what this thread brings of every tile: 16 channels of a key, 16 keys of a channel
   const int32_t* table = c.table + int64_t(i) * c.width;
@@ -180,33 +172,23 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
     }
   };
 
-  f32x16_t o[QT][MT];
-  float M[QT], l[QT];
+  f32x16_t o[MT];
+  float M = kNoKey, l = 0.f;
   float* row_lds = reinterpret_cast<float*>(buf + 2 * kBuf) + tid;
-  auto row = [&](int t, int what) -> float& { return row_lds[(what * QT + t) * kThreads]; };
+  auto row = [&](int what) -> float& { return row_lds[what * kThreads]; };
   // scales of k (their bits) from which on scores of the wave's rows may be large, or take the cap of large ones; 0 once a row has a reference
-  float most_unit = 0.f;
-#pragma unroll
-  for (int t = 0; t < QT; ++t) most_unit = fmaxf(most_unit, unit[t]);
+  float most_unit = fmaxf(0.f, qs.unit);
 #pragma unroll
   for (int k = 1; k < 32; k <<= 1) most_unit = fmaxf(most_unit, __shfl_xor(most_unit, k));
   const uint32_t near_scale = __builtin_amdgcn_readfirstlane(p.cap == kCapWide ? 1u : p.cap == kCapNear && p.cap_out <= kFar ? 0xFFFFFFFFu :
                                                              max(1u, __float_as_uint(near_factor(DB) / most_unit)));
   uint32_t far_scale = near_scale;
+  row(kFirstKey) = __int_as_float(klo);
+  row(kEndKey) = __int_as_float(khi);
+  row(kZeroMax) = kNoKey;
+  row(kZeroSum) = 0.f;
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    row(t, kFirstKey) = __int_as_float(klo[t]);
-    row(t, kEndKey) = __int_as_float(khi[t]);
-    row(t, kZeroMax) = kNoKey;
-    row(t, kZeroSum) = 0.f;
-  }
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    M[t] = kNoKey;
-    l[t] = 0.f;
-#pragma unroll
-    for (int m = 0; m < MT; ++m) o[t][m] = f32x16_t{};
-  }
+  for (int m = 0; m < MT; ++m) o[m] = f32x16_t{};
 
   if (begin < end) {
     pages_of(begin);
@@ -227,17 +209,13 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
     for (int n = 0; n < NT; ++n) {
       const int key0 = tile * KT + 32 * n;
       if (key0 >= whi || key0 + 32 <= wlo) continue;
-      f32x16_t x[QT];
-#pragma unroll
-      for (int t = 0; t < QT; ++t) x[t] = f32x16_t{};
+      f32x16_t x = f32x16_t{};
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         if (!EXACT && 16 * s >= d) continue;
         const half8_t k = now_buf[(2 * s + h) * kRunK + 32 * n + l32];
 #pragma unroll
-        for (int e = kParts - 1; e >= 0; --e)
-#pragma unroll
-          for (int t = 0; t < QT; ++t) x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[e][t][s], x[t], 0, 0, 0);
+        for (int e = kParts - 1; e >= 0; --e) x = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[e][s], x, 0, 0, 0);
       }
       // runs of 16 keys, results 0 .. 7 and 8 .. 15, which may be of two pages
       constexpr int kRuns = ONE ? 1 : 2, kRun = 16 / kRuns;
@@ -258,116 +236,113 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
           sc[k].inv *= __builtin_amdgcn_rcpf(sc[k].mant);
         }
       }
-      half8_t wt[kParts][QT][2];
+      half8_t wt[kParts][2];
+      float f[kRuns];
 #pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        float f[kRuns];
+      for (int k = 0; k < kRuns; ++k) f[k] = qs.unit * ksc[k];
+      if (p.cap == kCapNear) {
 #pragma unroll
-        for (int k = 0; k < kRuns; ++k) f[k] = unit[t] * ksc[k];
-        if (p.cap == kCapNear) {
+        for (int e = 0; e < 16; ++e) x[e] = capped<kF32>(x[e] * (f[e / kRun] * p.cap_in), p.cap_out);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[t][e] = capped<kF32>(x[t][e] * (f[e / kRun] * p.cap_in), p.cap_out);
-#pragma unroll
-          for (int k = 0; k < kRuns; ++k) f[k] = 1.f;
-        }
-        float top = kNoKey;
-        int from = 0, to = 0;
-        if (__builtin_expect(odd, 0)) {
-          from = __float_as_int(row(t, kFirstKey)) - key0 - 4 * h;
-          to = __float_as_int(row(t, kEndKey)) - key0 - 4 * h;
-        }
-        auto in = [&](int e) { return bool(int(8 * (e >> 2) + (e & 3) >= from) & int(8 * (e >> 2) + (e & 3) < to) & int(!gone[e / kRun])); };
-        if (__builtin_expect(!odd, 1)) {
-#pragma unroll
-          for (int k = 0; k < kRuns; ++k) {
-            float y = x[t][kRun * k];
-#pragma unroll
-            for (int e = 1; e < kRun; ++e) y = fmaxf(y, x[t][kRun * k + e]);
-            top = fmaxf(top, fmaf(y, f[k], sc[k].exp));
-          }
-        } else {
-          if (__builtin_expect(far, 0)) {
-            if (p.cap == kCapWide) {
-#pragma unroll
-              for (int e = 0; e < 16; ++e) x[t][e] = capped_wide(x[t][e] * (f[e / kRun] * p.cap_in), p.cap_out);
-#pragma unroll
-              for (int k = 0; k < kRuns; ++k) f[k] = 1.f;
-            }
-            float high = kNoKey;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) high = int(in(e)) & int(!sc[e / kRun].zero) ? fmaxf(high, x[t][e] * f[e / kRun]) : high;
-            const float old = far_scale == 0u ? row(t, kBase) : 0.f, base = next_base(other_half(high), old, M[t] == kNoKey);
-            M[t] = M[t] == kNoKey ? M[t] : M[t] + (old - base);
-            far_scale = __ballot(base != 0.f) ? 0u : near_scale;
-            if (far_scale == 0u) row(t, kBase) = base;
-            if (base != 0.f) {
-#pragma unroll
-              for (int e = 0; e < 16; ++e) x[t][e] = x[t][e] * f[e / kRun] - (sc[e / kRun].zero ? 0.f : base);
-#pragma unroll
-              for (int k = 0; k < kRuns; ++k) f[k] = 1.f;
-            }
-          }
-#pragma unroll
-          for (int k = 0; k < kRuns; ++k) {
-            float y = kNoKey;
-#pragma unroll
-            for (int e = kRun * k; e < kRun * k + kRun; ++e) y = in(e) ? fmaxf(y, x[t][e]) : y;
-            if (sc[k].zero) {
-              // keys of a page of zeros count in the sum of weights only, on a maximum of their own
-              float mz = row(t, kZeroMax), lz = row(t, kZeroSum);
-              const float most = fmaxf(mz, other_half(y == kNoKey ? y : y * f[k]));
-              lz *= __builtin_amdgcn_exp2f(mz - most);
-              mz = most;
-#pragma unroll
-              for (int e = kRun * k; e < kRun * k + kRun; ++e) lz += in(e) ? __builtin_amdgcn_exp2f(x[t][e] * f[k] - most) : 0.f;
-              row(t, kZeroMax) = mz;
-              row(t, kZeroSum) = lz;
-            } else {
-              top = y == kNoKey ? top : fmaxf(top, fmaf(y, f[k], sc[k].exp));
-            }
-          }
-        }
-        const float most = fmaxf(M[t], ceilf(other_half(top)) - kTop);
-        if (__ballot(most != M[t])) {
-          const float back = __builtin_amdgcn_exp2f(M[t] - most);
-          l[t] *= back;
-#pragma unroll
-          for (int m = 0; m < MT; ++m) o[t][m] *= back;
-          M[t] = most;
-        }
-        float P[16];
+        for (int k = 0; k < kRuns; ++k) f[k] = 1.f;
+      }
+      float top = kNoKey;
+      int from = 0, to = 0;
+      if (__builtin_expect(odd, 0)) {
+        from = __float_as_int(row(kFirstKey)) - key0 - 4 * h;
+        to = __float_as_int(row(kEndKey)) - key0 - 4 * h;
+      }
+      auto in = [&](int e) { return bool(int(8 * (e >> 2) + (e & 3) >= from) & int(8 * (e >> 2) + (e & 3) < to) & int(!gone[e / kRun])); };
+      if (__builtin_expect(!odd, 1)) {
 #pragma unroll
         for (int k = 0; k < kRuns; ++k) {
-          const float shift = sc[k].exp - M[t];
-          float sum = 0.f;
+          float y = x[kRun * k];
 #pragma unroll
-          for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] = __builtin_amdgcn_exp2f(fmaf(x[t][e], f[k], shift));
-          if (__builtin_expect(odd, 0)) {      // a scale that is no number must not reach keys that do not count
+          for (int e = 1; e < kRun; ++e) y = fmaxf(y, x[kRun * k + e]);
+          top = fmaxf(top, fmaf(y, f[k], sc[k].exp));
+        }
+      } else {
+        if (__builtin_expect(far, 0)) {
+          if (p.cap == kCapWide) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = capped_wide(x[e] * (f[e / kRun] * p.cap_in), p.cap_out);
+#pragma unroll
+            for (int k = 0; k < kRuns; ++k) f[k] = 1.f;
+          }
+          float high = kNoKey;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) high = int(in(e)) & int(!sc[e / kRun].zero) ? fmaxf(high, x[e] * f[e / kRun]) : high;
+          const float old = far_scale == 0u ? row(kBase) : 0.f, base = next_base(other_half(high), old, M == kNoKey);
+          M = M == kNoKey ? M : M + (old - base);
+          far_scale = __ballot(base != 0.f) ? 0u : near_scale;
+          if (far_scale == 0u) row(kBase) = base;
+          if (base != 0.f) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = x[e] * f[e / kRun] - (sc[e / kRun].zero ? 0.f : base);
+#pragma unroll
+            for (int k = 0; k < kRuns; ++k) f[k] = 1.f;
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < kRuns; ++k) {
+          float y = kNoKey;
+#pragma unroll
+          for (int e = kRun * k; e < kRun * k + kRun; ++e) y = in(e) ? fmaxf(y, x[e]) : y;
+          if (sc[k].zero) {
+            // keys of a page of zeros count in the sum of weights only, on a maximum of their own
+            float mz = row(kZeroMax), lz = row(kZeroSum);
+            const float most = fmaxf(mz, other_half(y == kNoKey ? y : y * f[k]));
+            lz *= __builtin_amdgcn_exp2f(mz - most);
+            mz = most;
+#pragma unroll
+            for (int e = kRun * k; e < kRun * k + kRun; ++e) lz += in(e) ? __builtin_amdgcn_exp2f(x[e] * f[k] - most) : 0.f;
+            row(kZeroMax) = mz;
+            row(kZeroSum) = lz;
+          } else {
+            top = y == kNoKey ? top : fmaxf(top, fmaf(y, f[k], sc[k].exp));
+          }
+        }
+      }
+      const float most = fmaxf(M, ceilf(other_half(top)) - kTop);
+      if (__ballot(most != M)) {
+        const float back = __builtin_amdgcn_exp2f(M - most);
+        l *= back;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) o[m] *= back;
+        M = most;
+      }
+      float P[16];
+#pragma unroll
+      for (int k = 0; k < kRuns; ++k) {
+        const float shift = sc[k].exp - M;
+        float sum = 0.f;
+#pragma unroll
+        for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] = __builtin_amdgcn_exp2f(fmaf(x[e], f[k], shift));
+        if (__builtin_expect(odd, 0)) {      // a scale that is no number must not reach keys that do not count
+#pragma unroll
+          for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] = int(in(e)) & int(!sc[k].zero) ? P[e] : 0.f;
+        }
+#pragma unroll
+        for (int e = kRun * k; e < kRun * k + kRun; ++e) sum += P[e];
+        if constexpr (kF32) {
+#pragma unroll
+          for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] *= sc[k].mant;
+          if (__builtin_expect(odd, 0)) {
 #pragma unroll
             for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] = int(in(e)) & int(!sc[k].zero) ? P[e] : 0.f;
           }
-#pragma unroll
-          for (int e = kRun * k; e < kRun * k + kRun; ++e) sum += P[e];
-          if constexpr (kF32) {
-#pragma unroll
-            for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] *= sc[k].mant;
-            if (__builtin_expect(odd, 0)) {
-#pragma unroll
-              for (int e = kRun * k; e < kRun * k + kRun; ++e) P[e] = int(in(e)) & int(!sc[k].zero) ? P[e] : 0.f;
-            }
-          }
-          l[t] = sum == 0.f ? l[t] : fmaf(sum, sc[k].inv, l[t]);      // (nothing times a scale that is no number is nothing)
         }
+        l = sum == 0.f ? l : fmaf(sum, sc[k].inv, l);      // (nothing times a scale that is no number is nothing)
+      }
 #pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-          const half2_t y = to_half(P[e], P[e + 1]);
-          wt[0][t][e >> 3][e & 7] = y[0];
-          wt[0][t][e >> 3][(e & 7) + 1] = y[1];
-          if constexpr (kF32) {
-            const half2_t rest = to_half(P[e] - float(y[0]), P[e + 1] - float(y[1]));
-            wt[1][t][e >> 3][e & 7] = rest[0];
-            wt[1][t][e >> 3][(e & 7) + 1] = rest[1];
-          }
+      for (int e = 0; e < 16; e += 2) {
+        const half2_t y = to_half(P[e], P[e + 1]);
+        wt[0][e >> 3][e & 7] = y[0];
+        wt[0][e >> 3][(e & 7) + 1] = y[1];
+        if constexpr (kF32) {
+          const half2_t rest = to_half(P[e] - float(y[0]), P[e + 1] - float(y[1]));
+          wt[1][e >> 3][e & 7] = rest[0];
+          wt[1][e >> 3][(e & 7) + 1] = rest[1];
         }
       }
 #pragma unroll
@@ -377,9 +352,7 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
           if (!EXACT && 32 * m >= d) continue;
           const half8_t v = now_buf[kBufK + (2 * (2 * n + u) + h) * kRunV + 32 * m + l32];
 #pragma unroll
-          for (int e = kParts - 1; e >= 0; --e)
-#pragma unroll
-            for (int t = 0; t < QT; ++t) o[t][m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, wt[e][t][u], o[t][m], 0, 0, 0);
+          for (int e = kParts - 1; e >= 0; --e) o[m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, wt[e][u], o[m], 0, 0, 0);
         }
     }
     if (tile + 1 < end) put(buf + ((tile + 1 - begin) & 1) * kBuf);
@@ -387,26 +360,23 @@ __global__ __launch_bounds__(64 * many_waves(Tag::dtype, DB), many_resident(Tag:
   }
 
   const int64_t part = ((w * c.heads + head) * p.splits + split) * kTile;
+  const int place = wave * 32 + l32, R = first + place;
+  float sum = l + __shfl_xor(l, 32), lz = row(kZeroSum), sumz = lz + __shfl_xor(lz, 32), mz = row(kZeroMax);
+  const Finish fin = finish_of(M, far_scale == 0u ? row(kBase) : 0.f);
+  const float both = fmaxf(fin.all, mz), near = __builtin_amdgcn_exp2f(fin.all - both), own = fin.unit * near;
+  const float total = sum * (fin.sum_unit * near) + sumz * __builtin_amdgcn_exp2f(mz - both);
+  if (R >= r.rows) return;
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const int place = wave * 32 * QT + 32 * t + l32, R = first + place;
-    float sum = l[t] + __shfl_xor(l[t], 32), lz = row(t, kZeroSum), sumz = lz + __shfl_xor(lz, 32), mz = row(t, kZeroMax);
-    const Finish fin = finish_of(M[t], far_scale == 0u ? row(t, kBase) : 0.f);
-    const float both = fmaxf(fin.all, mz), near = __builtin_amdgcn_exp2f(fin.all - both), own = fin.unit * near;
-    const float total = sum * (fin.sum_unit * near) + sumz * __builtin_amdgcn_exp2f(mz - both);
-    if (R >= r.rows) continue;
+  for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        const int ch = 32 * m + 2 * e + 4 * h;
-        if (!EXACT && ch >= d) continue;
-        const f32x4_t v = f32x4_t{o[t][m][e], o[t][m][e + 1], o[t][m][e + 2], o[t][m][e + 3]} * own;
-        if (used > 1) *reinterpret_cast<f32x4_t*>(p.parts + (part + place) * d + ch) = v;
-        else store_row<Tag>(p, r, R, head, ch, v, both, total);
-      }
-    if (used > 1 && h == 0) *reinterpret_cast<float2*>(p.sums + 2 * (part + place)) = make_float2(both, total);
-  }
+    for (int e = 0; e < 16; e += 4) {
+      const int ch = 32 * m + 2 * e + 4 * h;
+      if (!EXACT && ch >= d) continue;
+      const f32x4_t v = f32x4_t{o[m][e], o[m][e + 1], o[m][e + 2], o[m][e + 3]} * own;
+      if (used > 1) *reinterpret_cast<f32x4_t*>(p.parts + (part + place) * d + ch) = v;
+      else store_row<Tag>(p, r, R, head, ch, v, both, total);
+    }
+  if (used > 1 && h == 0) *reinterpret_cast<float2*>(p.sums + 2 * (part + place)) = make_float2(both, total);
 }
 
 // The parts of a tile's rows joined in their order, four channels a thread.
