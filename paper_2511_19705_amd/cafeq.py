@@ -10,6 +10,7 @@ import ctypes
 import functools
 import math
 import os
+import struct
 from typing import NamedTuple, Optional
 
 import torch
@@ -97,6 +98,9 @@ class Attention(ctypes.Structure):
                 ("scale", ctypes.c_float), ("softcap", ctypes.c_float)]
 
 
+_pack_attention = struct.Struct("@PPPqqqqqqPiiiiff").pack      # an Attention's bytes, in a quarter of the time
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise CafeqError("libcafeq.so has not been built (run `python __graft_entry__.py`): " + LIB_PATH)
@@ -156,8 +160,8 @@ def _load():
     lib.cafeq_rotate_heads.argtypes = [ctypes.POINTER(Rotation), ctypes.POINTER(Heads), ctypes.POINTER(Heads), i64, vp, vp, vp]
     lib.cafeq_cache_append.argtypes = [cache, vp, vp, i32, i64, i64, i64, i64, i64, vp, i64, vp]
     lib.cafeq_cache_values.argtypes = [cache, vp, vp, i64, vp, vp, i32, vp]
-    lib.cafeq_cache_attend.argtypes = [cache, ctypes.POINTER(Attention), vp, vp]
-    lib.cafeq_cache_attend_workspace_bytes.argtypes = [cache, ctypes.POINTER(Attention)]
+    lib.cafeq_cache_attend.argtypes = [cache, vp, vp, vp]      # (an Attention, or its bytes)
+    lib.cafeq_cache_attend_workspace_bytes.argtypes = [cache, vp]
     lib.cafeq_cache_reserve.argtypes = [cache, vp, i64, vp, vp, vp, vp]
     lib.cafeq_cache_reorder.argtypes = [cache, vp, vp, vp]
     lib.cafeq_cache_compact.argtypes = [cache, vp, vp, vp]
@@ -831,8 +835,8 @@ def kv_cache(sequences, pages, heads, d, block=64, width=None, device=None):
 
 
 def _cache(c, dev):
-    """(descriptor, its reference for a call, device, scratch of the page calls, what the tensors were) of a KVCache on device number `dev`.  The checks of
-    eight tensors (8 us) are made once, and again where one has another address, shape or order."""
+    """(descriptor, its reference for a call, device, scratch of the page calls, what the tensors were, scratch of attention by its sizes) of a KVCache on
+    device number `dev`.  The checks of eight tensors (8 us) are made once, and again where one has another address, shape or order."""
     have = c._desc
     k, v, ks, vs, table, lengths, refs, missing = c.k, c.v, c.kscale, c.vscale, c.table, c.lengths, c.refs, c.missing
     at = (k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), table.data_ptr(), lengths.data_ptr(), refs.data_ptr(), missing.data_ptr(), k.shape, v.shape,
@@ -849,7 +853,7 @@ def _cache(c, dev):
                  _operand(ks, dev, f32, (pages, heads), "cache.kscale"), _operand(vs, dev, f32, (pages, heads), "cache.vscale"),
                  _operand(table, dev, i32, (rows, width), "cache.table"), _operand(lengths, dev, i32, (rows,), "cache.lengths"),
                  _operand(refs, dev, i32, (pages,), "cache.refs"), pages, rows, width, heads, d, block, _operand(missing, dev, i32, (1,), "cache.missing"))
-    have = (desc, ctypes.byref(desc), dev, int(lib.cafeq_cache_pages_workspace_bytes(ctypes.byref(desc))), at)
+    have = (desc, ctypes.byref(desc), dev, max(256, int(lib.cafeq_cache_pages_workspace_bytes(ctypes.byref(desc)))), at, {})
     object.__setattr__(c, "_desc", have)
     return have
 
@@ -909,7 +913,7 @@ def cache_attend(cache, q, starts, longest=None, scale=None, softcap=0.0, window
     dev, kind = torch._C._cuda_getDevice(), _FLOATS.get(q.dtype)
     if kind is None:
         raise CafeqError("q must be float32 or bfloat16")
-    c, ref = _cache(cache, dev)[:2]
+    c, ref, _, _, _, sizes = _cache(cache, dev)
     shape = q.shape
     n, hq, d = shape if len(shape) == 3 else (0, 0, 0)
     if d != c.d or hq < 1 or hq % c.heads:
@@ -925,17 +929,25 @@ def cache_attend(cache, q, starts, longest=None, scale=None, softcap=0.0, window
             raise CafeqError("out must have the shape and type of q")
         ldo, hso = _head_rows(out, dev, "out")
     sums = torch.empty((n, hq), dtype=torch.float32, device=q.device) if lse else None
-    a = Attention(q.data_ptr(), out.data_ptr(), None if sums is None else sums.data_ptr(), n, ldq, hsq, ldo, hso, _bound(longest, n),
-                  _starts(starts, c.sequences, dev), kind, hq, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, softcap)
+    longest = _bound(longest, n)
+    a = _pack_attention(q.data_ptr(), out.data_ptr(), 0 if sums is None else sums.data_ptr(), n, ldq, hsq, ldo, hso, longest,
+                        _starts(starts, c.sequences, dev), kind, hq, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, softcap)
     if n:
         stream = torch._C._cuda_getCurrentRawStream(dev)
-        pa = ctypes.byref(a)
-        nbytes = lib.cafeq_cache_attend_workspace_bytes(ref, pa)
+        key = (kind, n, hq, longest, window, causal)
+        nbytes = sizes.get(key)
+        known = nbytes is not None
+        if not known:
+            nbytes = lib.cafeq_cache_attend_workspace_bytes(ref, a)
         # the buffer is of this call alone, so that streams share nothing
         ws = q.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
-        rc = lib.cafeq_cache_attend(ref, pa, _ptr(ws), stream)      # (held until the launch is made: another thread may allocate)
+        rc = lib.cafeq_cache_attend(ref, a, _ptr(ws), stream)      # (held until the launch is made: another thread may allocate)
         if rc:
             _check(rc)
+        if not known:      # of calls that are refused the size says nothing
+            if len(sizes) > 63:
+                sizes.clear()
+            sizes[key] = nbytes
     return (out, sums) if lse else out
 
 
@@ -947,8 +959,8 @@ class Reserved(NamedTuple):
 
 def _pages_call(cache):
     dev = torch._C._cuda_getDevice()
-    c, ref, _, nbytes, _ = _cache(cache, dev)
-    return dev, c, ref, cache.k.new_empty(max(256, nbytes), dtype=torch.uint8), torch._C._cuda_getCurrentRawStream(dev)
+    c, ref, _, nbytes, _, _ = _cache(cache, dev)
+    return dev, c, ref, cache.k.new_empty(nbytes, dtype=torch.uint8), torch._C._cuda_getCurrentRawStream(dev)
 
 
 def cache_reserve(cache, starts, n):
@@ -957,7 +969,9 @@ def cache_reserve(cache, starts, n):
     cache_append stores nothing and cache_attend returns zeros."""
     dev, c, ref, ws, stream = _pages_call(cache)
     positions, missing = cache.refs.new_empty(n), cache.refs.new_empty(1)
-    _check(lib.cafeq_cache_reserve(ref, _starts(starts, c.sequences, dev), n, positions.data_ptr() if n else None, missing.data_ptr(), ws.data_ptr(), stream))
+    rc = lib.cafeq_cache_reserve(ref, _starts(starts, c.sequences, dev), n, positions.data_ptr() if n else None, missing.data_ptr(), ws.data_ptr(), stream)
+    if rc:
+        _check(rc)
     return Reserved(positions, missing)
 
 

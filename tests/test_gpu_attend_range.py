@@ -91,3 +91,18 @@ def test_many_keys_of_equal_weight_at_the_ends_of_the_scales(env, dtype, power):
             for g in (2 * h, 2 * h + 1):
                 tol = (2.0 ** -14 if dtype == "f32" else 2.0 ** -11 + 2.0 ** -14) * W + (0.0 if dtype == "f32" else 2.0 ** -8) * want.abs()
                 assert ((out[:, g].double() - want).abs() <= tol).all()
+
+
+def test_a_refused_call_leaves_nothing_behind(env):
+    """The scratch of a call is known by its sizes; a call of these sizes that is refused needs none, the next one of them does."""
+    torch, cafeq = env
+    for counts in ([1, 1], [90, 2]):
+        cache, q, starts = _problem(env, counts, [3000, 2000])
+        apart = torch.zeros((sum(counts), 4 * 64 + 1), device="cuda:0", dtype=q.dtype)[:, :256].unflatten(1, (4, 64))
+        for bad in (dict(out=q), dict(softcap=-1.0), dict(out=apart)):
+            with pytest.raises(cafeq.CafeqError):
+                cafeq.cache_attend(cache, q, starts, **bad)
+        want = cafeq.cache_attend(cache, q, starts)
+        for i in range(70):      # more sizes than are kept
+            cafeq.cache_attend(cache, q, starts, window=1 + i)
+        assert torch.equal(cafeq.cache_attend(cache, q, starts), want)
