@@ -286,7 +286,8 @@ int cafeq_infer_packed(const void* X, int x_type, int64_t n, int64_t ldx, const 
  *   pairs (a, b) of the first `rot` channels -> amplitude (a cos w - b sin w, a sin w + b cos w), w = positions[t] freq[i],
  *   pair i being channels (i, i + rot/2), or (2i, 2i + 1) with interleaved; the other channels stay y.
  * freq: rot/2 float64 in radians a position; the angle is formed and reduced in float64 (float32 loses it at far positions), the
- * rest is float32, one rounding to dtype (float32 or bfloat16).  positions int32 [n].  d even, up to 512; rot even, 0 .. d.
+ * rest is float32, one rounding to dtype (float32 or bfloat16; for bfloat16 sine and cosine are good to 2^-20, which shows only where a pair cancels).
+ * positions int32 [n].  d even, up to 512; rot even, 0 .. d.
  * Any strides and alignments (d, rot, ld and hs multiples of 8 with 16-byte aligned pointers are faster).  out may be x itself
  * with the same strides, and overlaps no input otherwise.  Either part may be absent (x NULL).  n up to 2^21, heads up to 4096. */
 typedef struct {
@@ -348,13 +349,16 @@ int cafeq_cache_values(const cafeq_cache* cache, const int32_t* begin, const int
  * head h reads key head h / (heads_q / heads):
  *   x_t = scale q . K_t, with 0 < softcap <= 2^100: softcap tanh(x_t / softcap);  keys t: 0 <= t < lengths[i], t <= p if causal, t > p - window if window > 0
  *   out = sum_t exp(x_t) V_t / sum_t exp(x_t),  lse = log sum_t exp(x_t)   (a row without keys: 0 and -inf)
- * Scores are float32 numbers of any magnitude up to 2^126 (a row whose largest passes 2^126 is not specified); from 2^12 on a row may take them against a whole number near its largest.
+ * Scores are float32: any, as long as |scale| max|q| max|K| d stays below 2^126 (beyond it a row is not specified).
  * K, V: the codes times their scales, which are not negative.  q, out float32 or bfloat16 (dtype); lse float32 [n][heads_q] dense or NULL.  Queries of bfloat16 are
- * taken exactly (magnitudes below 2^-28 of the row's largest to multiples of 2^-39 of it), probabilities rounded to 11 bits (below 2^-28 of the
- * largest, weighed with the scale of v, to multiples of 2^-39 of it); with float32 both are taken in two such parts.  Sums are float32 in a fixed order.  A row of q that holds a NaN or an infinity gives NaN.  A page and head of v with a scale below 2^-100 counts as zeros;
- * where scales of a head lie more than 2^100 apart the weight of the smaller ones' keys may be lost.
+ * taken exactly (magnitudes below 2^-31 of the row's largest to multiples of 2^-38 of it), probabilities rounded to 11 bits (below 2^-27 of the
+ * largest, weighed with the scale of v, to multiples of 2^-37 of it); with float32 both are taken in two such parts.  A soft cap on bfloat16 is good to 2^-22 of
+ * the cap, and above 256 to 2^-20 of the score.  Sums are float32 in an order that follows from the sizes (the table's width, sequences, n and longest), so that
+ * the same keys in a wider table may round otherwise in the last bits.  A row of q that holds a NaN or an infinity gives NaN.  A page and
+ * head of v with a scale below 2^-100 counts as zeros; where scales of a head lie more than 2^100 apart the weight of the smaller ones' keys may be lost.
  * Rows start at multiples of 16 bytes; out overlaps no input.  longest as in cafeq_cache_append (rows beyond it are left).
- * heads_q a multiple of heads, up to 4096; n up to 2^24, n * heads_q below 2^31, and what a launch holds: 2 n heads_q + 512 sequences heads below 2^32 is always taken.  ws: cafeq_cache_attend_workspace_bytes() bytes (may be 0), 16-byte aligned. */
+ * heads_q a multiple of heads, up to 4096; n up to 2^24, n * heads_q below 2^31, and what a launch holds (2 n heads_q + 512 sequences heads below 2^32 is
+ * always taken).  ws: cafeq_cache_attend_workspace_bytes() bytes (may be 0), 16-byte aligned. */
 typedef struct {
   const void* q;
   void* out;
@@ -371,7 +375,8 @@ int cafeq_cache_attend(const cafeq_cache* cache, const cafeq_attention* a, void*
  * the cache on another stream meanwhile.  ws: cafeq_cache_pages_workspace_bytes(cache) bytes, 16-byte aligned.
  * reserve: room for starts[i+1] - starts[i] more tokens of each sequence.  Row by row the lowest free pages (refs 0) are taken: first, where the
  *   sequence's last page is partly filled and refs of it exceed 1, one that the page is copied to and that takes its place, then
- *   one for each new block.  lengths grow, refs follow.  positions (int32 [n] or NULL): the position of every new token.  missing
+ *   one for each new block.  lengths grow, refs follow.  (Whoever shortens a sequence by its length alone has to let the pages behind it go too:
+ *   table -1, refs less one.)  positions (int32 [n] or NULL): the position of every new token.  missing
  *   (int32 [1], and the cache's): 0, or how many pages or table columns lack; then nothing is changed, and positions are 0.
  * reorder: row i takes over what row sources[i] held before the call (sources int32 [sequences], any value outside [0, sequences): nothing; the row's own number: it
  *   stays).  The same source may be given several times: pages are shared, refs count their rows.  Pages that no row holds any more are free.

@@ -6,8 +6,8 @@
 //
 // A page's scale of v, mant 2^exp, goes into the exponent: with y = x + exp (x the score in units of log2) and M the largest y so far, rounded up, less 14,
 //   p = 2^(y - M) <= 2^14,   out = sum p mant c_v / sum p 2^-exp.
-// What is rounded to float16, p mant (to 11 bits down to 2^-28 of the largest), so is weighed as it counts in the result, however scales differ from page to page; and exp - M is a whole
-// number, so that the exponent's argument takes one rounding, in proportion to itself.
+// What is rounded to float16, p mant in (2^13, 2^15) for the largest (to 11 bits down to 2^-27 of it, to multiples of 2^-37 of it below), so is weighed as it counts in the
+// result, however scales differ from page to page; and exp - M is a whole number, so that the exponent's argument takes one rounding, in proportion to itself.
 #pragma once
 #include "cache.hpp"
 
@@ -117,7 +117,7 @@ __device__ __forceinline__ Finish finish_of(float M, float base) {
 }
 
 // Rows of q are taken times a power of two that brings the largest magnitude (its bits) to [2^14, 2^15): bfloat16 then is exact in float16 down to
-// 2^-28 of it.  unit: what a product's sum is times, next to the scale of k, in the score (in log2 without a soft cap)
+// 2^-31 of it.  unit: what a product's sum is times, next to the scale of k, in the score (in log2 without a soft cap)
 struct QueryScale { float up, unit; };
 __device__ __forceinline__ QueryScale query_scale(uint32_t bits, const cafeq_attention& a) {
   const int e = max(-100, int(bits >> 23) - 127);
@@ -128,7 +128,7 @@ __device__ __forceinline__ QueryScale query_scale(uint32_t bits, const cafeq_att
   return s;
 }
 
-// Many rows, by 64 channels (db): keys of a tile, waves of a workgroup (32 rows each), waves a SIMD that registers and LDS allow.  A prompt of 8192, TFLOP/s:
+// Many rows, by 64 channels (db): keys of a tile, waves of a workgroup (32 rows each), waves a SIMD that registers and LDS allow.  A prompt of 8192, TFLOP/s of the first form:
 // 8 heads of 256, 4 waves and 32 keys 675, 8 and 32 817, 8 and 64 856; 16 heads of 128, 4 and 64 817, 8 and 64 849, 4 and 32 (three waves a SIMD) 861, 8 and 128 784;
 // 4 heads of 64, 4 and 64 637, 8 and 64 569; in float32 16 heads of 128, 4 and 32 438, 4 and 64 450, 8 and 64 491.
 constexpr int many_keys(int dtype, int db) { return db == 2 && dtype != CAFEQ_F32 ? 32 : dtype == CAFEQ_F32 && db > 2 ? 32 : 64; }

@@ -26,9 +26,10 @@ __device__ __forceinline__ float sum_across(float v) {
 // 16x16x32, has the keys of g = r / 4, 4 t + r % 4 of them, in row r, so that a lane's results are the eight keys whose weights it gives to the second
 // product.  Codes go from memory to registers, 16 bytes a lane: of k the channels 16 g .. of a key, of v the 16 keys of a run for one channel, of
 // which two tiles of 16 channels swap halves between lanes.  The next step's of k are on their way while this one is worked on.
-// Bound by memory: 48 sequences of 1600 to 32700 keys, 16 heads of 128, 617 us, 5.4 TB/s (a copy reaches 4.9, reading alone 6.7); one of 131072 110, 4.9 TB/s; 48 of
-// 8192, 8 heads of 256, 285, 5.7 TB/s.  Short sequences by what has to follow each other (lengths and pages, codes, two products, the join): 512 keys of 4 heads of
-// 256 7.9, and 3.7 for the join.  The rows in LDS and 16 KB of codes a wave at once keep two waves a SIMD at any d.
+// Bound by memory: 48 sequences of 1600 to 32700 keys, 16 heads of 128, 618 us, 5.4 TB/s (a copy reaches 4.9, reading alone 6.7); one of 131072 109, 4.9 TB/s; 48 of
+// 8192, 8 heads of 256, 300, 5.4 TB/s.  Short sequences by what has to follow each other (lengths and pages, codes, two products, the join): 512 keys of 4 heads of
+// 256 8.1, and 3.8 for the join.  The rows in LDS and 16 KB of codes a wave at once (8 KB for d of 80, 96 and 112, whose registers are the general form's) keep two waves a
+// SIMD, for float32 with d above 192 one.
 template <class Tag, int DB, bool EXACT>
 __global__ __launch_bounds__(kThreads, Tag::dtype == CAFEQ_F32 && DB == 4 ? 1 : 2) void attend_few_kernel(const AttendPlan p) {
   using elem = typename Tag::elem;

@@ -23,9 +23,10 @@ __device__ __forceinline__ float lane_value(float v, int lane) { return __uint_a
 // and of 32 keys those with key / 4 % 2 = l / 32: results i of a product are keys 8 (i / 4) + 4 (l / 32) + i % 4, weights 8 u .. 8 u + 7 what it gives to step u of
 // the second product.  LDS: K as [16 channels][half][key], V as [16 keys][half][channel] of eight float16 each, a place of 16 bytes
 // behind every run so that lanes that write side by side hit different banks.  Two buffers: the next tile's codes are on their way while this one is multiplied.
-// Bound by vector instructions next to the matrix instructions (the exponentials above all: a quarter of the rate, two and a reciprocal with a soft cap): a prompt of 8192,
-// 8 heads of 256, 16 query heads 643 us, 856 TFLOP/s, with a soft cap 742; 16 heads of 128, 32 query heads 650, 845 TFLOP/s; a product of 8192^3 reaches 1360.
-// Counted while pages were looked up by every thread: matrix pipe busy 27 %, vector instructions issued in half of the cycles, LDS active in 24 %.  Raised priority around
+// Bound by what a wave does one after another: products, exponentials (at a quarter of the rate, two and a reciprocal with a soft cap), reads of LDS: a prompt of 8192,
+// 8 heads of 256, 16 query heads 667 us, 824 TFLOP/s, with a soft cap 758 (replayed on one state; 803 on three in turn); 16 heads of 128, 32 query heads 643, 855 TFLOP/s; a product of
+// 8192^3 reaches 1360.  Counted: of heads of 256 with a cap the matrix pipe is busy 32 % of the time, vector instructions issue in 40 % (exponentials and reciprocals take four times as
+// long), LDS is active in 22 %; of heads of 128 39, 63 and 40 %.  Nothing is saturated: waves leave a barrier in step, and what they do adds up.  Raised priority around
 // the matrix instructions, or around the rest, made it 5 to 18 % slower; operands read four steps ahead nothing; 64 rows a wave (half the LDS reads) spilled.
 // ONE: a tile's keys are of one page.
 template <class Tag, int DB, bool EXACT, bool ONE>
