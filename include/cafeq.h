@@ -311,7 +311,8 @@ int cafeq_rotate_heads(const cafeq_rotation* cfg, const cafeq_heads* q, const ca
  * [sequences][width]: the page of each block of a sequence (blocks behind its length: -1); lengths [sequences]: its tokens;
  * refs [pages]: rows of the table that hold a page (0: free; used by reserve, reorder and compact only).  missing: what the last
  * cafeq_cache_reserve lacked, which alone writes it (0 at first).  While it is not 0 append stores nothing, and attend takes no token as a key
- * (rows are 0, lse -inf): steps that find no room, in a captured graph too, leave the cache as it is.  With NULL the caller sees to that.  All device memory, owned by the
+ * (rows are 0, lse -inf): steps that find no room, in a captured graph too, leave the cache as it is, until a reserve finds room, be it for no token.  With NULL the
+ * caller sees to that.  All device memory, owned by the
  * caller; k and v 16-byte aligned.  d a multiple of 16 up to 256, block 16, 32, 64 or 128, pages * heads up to 2^31 - 1, heads up to 4096,
  * width * block up to 2^30, sequences up to 65535.  Numbers in device memory are not trusted with addresses: lengths beyond width * block count as
  * that, and tokens whose page is outside [0, pages) are not read or written and are no keys. */

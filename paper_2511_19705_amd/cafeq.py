@@ -966,7 +966,7 @@ def _pages_call(cache):
 def cache_reserve(cache, starts, n):
     """cafeq_cache_reserve: room for starts[i + 1] - starts[i] more tokens of each sequence, n in all.  Nothing waits: a caller that cannot be
     sure of room reads `missing` (one int32 on the device); where it is not 0 nothing has changed, positions are 0, and until a reserve finds room
-    cache_append stores nothing and cache_attend returns zeros."""
+    (for no token: starts of zeros) cache_append stores nothing and cache_attend returns zeros."""
     dev, c, ref, ws, stream = _pages_call(cache)
     positions, missing = cache.refs.new_empty(n), cache.refs.new_empty(1)
     rc = lib.cafeq_cache_reserve(ref, _starts(starts, c.sequences, dev), n, positions.data_ptr() if n else None, missing.data_ptr(), ws.data_ptr(), stream)

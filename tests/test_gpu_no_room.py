@@ -123,3 +123,15 @@ def test_without_a_place_for_it(env):
     ws = torch.empty(max(16, cafeq.lib.cafeq_cache_attend_workspace_bytes(ctypes.byref(desc), ctypes.byref(a))), dtype=torch.uint8, device="cuda:0")
     assert cafeq.lib.cafeq_cache_attend(ctypes.byref(desc), ctypes.byref(a), ws.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
     assert torch.equal(out, want)
+
+
+def test_a_reserve_for_no_token_opens_the_cache(env):
+    torch, cafeq = env
+    cache = cafeq.kv_cache(1, 2, H, D, block=B)
+    _step(env, cache, _x(env, 30, torch.float32), _ints(torch, [0, 30]), 30, 30)
+    q, s = torch.randn((1, HQ, D), device="cuda:0"), _ints(torch, [0, 1])
+    want = cafeq.cache_attend(cache, q, s)
+    assert int(cafeq.cache_reserve(cache, _ints(torch, [0, 9]), 9).missing) == 1
+    assert (cafeq.cache_attend(cache, q, s) == 0).all()
+    assert int(cafeq.cache_reserve(cache, _ints(torch, [0, 0]), 0).missing) == 0
+    assert torch.equal(cafeq.cache_attend(cache, q, s), want) and cache.lengths.tolist() == [30]
